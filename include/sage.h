@@ -322,6 +322,81 @@ int sage_topm(const float* alpha, int64_t N, int64_t m, int64_t* out_idx, void* 
 #define SAGE_TOPM_STATIC_MAX_N 16777216
 int sage_topm_static(const float* alpha, int64_t N, int64_t m, int64_t* out_idx, void* hip_stream);
 
+/* ---- around a head: labels for its rows, their errors, the update of its weights -------------------------------- */
+
+/*
+ * A label for every row of logits, drawn from the row's own distribution with a given random number: for examples that
+ * have none (gradients of drawn labels are rows of the Fisher matrix), and, one row at a time, for serving.
+ *
+ * logits: DEVICE, row i starts at element i * ld, ld >= n_classes; columns behind the classes are not read. u: DEVICE, one fp32 per
+ * row in [0, 1). labels: DEVICE, receives one int32 per row. logp: DEVICE, receives the label's log-probability under the
+ * distribution it was drawn from, or NULL. 1 <= n_classes <= SAGE_MAX_CLASSES.
+ *
+ * The weight of class j is the whole number w_j = rint(2^42 exp((z_j - max z) / temperature)), 0 where z_j = -inf. Classes are
+ * ordered by z descending, of equals the lower index first, and reduced in this order:
+ *   top_k  > 0: the first top_k of them (0 or less, n_classes or more: all);
+ *   top_p  < 1: with S the sum of the kept weights, the first, and every further one before which the kept weights sum to less than
+ *               ceil(top_p * S) (NaN: all);
+ *   min_p  > 0: those with z_j - max z >= temperature * ln(min(min_p, 1)).
+ * With S the sum of what is left and t = min(floor(u * S), S - 1) the label is the first class, by index, up to which the kept
+ * weights sum to more than t. Equal rows and numbers give equal labels, whatever else is in the batch. A u below 0 (or NaN) counts
+ * as 0, one of 1 or more takes the last kept class with a weight.
+ * temperature <= 0 or NaN: the class of the greatest logit, the lowest of equals, with logp 0. A row that has no greatest finite
+ * logit (all -inf, or a NaN or +inf in it): label -1, logp NaN; sage_logit_error takes -1 for no label.
+ *
+ * how: HOST, or NULL for { 1, 0, 1, 0 } without arrays. Each *_rows: DEVICE, one value per row, or NULL: the value beside it
+ * holds for all rows. Asynchronous on hip_stream; allocates nothing and may be captured in a graph.
+ */
+#define SAGE_MAX_CLASSES 1048576
+typedef struct {
+    float temperature;
+    int32_t top_k;
+    float top_p;
+    float min_p;
+    const float* temperature_rows;
+    const int32_t* top_k_rows;
+    const float* top_p_rows;
+    const float* min_p_rows;
+} sage_sampling;
+int sage_sample(const void* logits, sage_dtype dtype, int64_t rows, int64_t n_classes, int64_t ld, const float* u,
+                const sage_sampling* how, int32_t* labels, float* logp, void* hip_stream);
+
+/*
+ * The cross-entropy of every row of logits with its label, and its gradient with respect to the logits: the factor E of
+ * sage_fd_update_outer and its like (Method, definition of g_i, for a linear head), and of a training step the loss and the backward
+ * pass at once:
+ *     loss_i = ln sum_j exp(z_ij) - z_iy,      E_ij = weights_i * (exp(z_ij) / sum_l exp(z_il) - [j = y]).
+ * logits as for sage_sample. labels: DEVICE, one int32 y per row; a row with y < 0 has none: loss 0, E zero. y >= n_classes: loss and
+ * E are NaN. weights: DEVICE, one fp32 per row (the gradient of whatever is made of the losses), or NULL: 1. E: DEVICE, row i
+ * starts at element i * ld_e, of type e_dtype; may be the logits' own memory if type and ld are theirs, and must not overlap it
+ * otherwise (SAGE_ERR_ARG); or NULL. loss: DEVICE, one fp32 per row, or NULL. Columns behind the classes are neither read nor
+ * written. Sums are fp32; E_iy is formed from the other classes' sum, so that it keeps its digits where the label's probability
+ * is nearly 1. Logits of -inf have probability 0; a label among them has an infinite loss; a row of nothing else has an infinite loss
+ * and E zero. A NaN or +inf in a row with a label makes its loss and E NaN. Asynchronous on hip_stream; allocates nothing.
+ */
+int sage_logit_error(const void* logits, sage_dtype dtype, int64_t rows, int64_t n_classes, int64_t ld, const int32_t* labels,
+                     const float* weights, void* E, sage_dtype e_dtype, int64_t ld_e, float* loss, void* hip_stream);
+
+/*
+ * Matrices made orthogonal by Newton-Schulz products, as the update of a weight matrix from its gradient (of the kept rows, say):
+ *     X = G / (||G||_F + eps);   then, for each of the steps, with A = X X^T:   X <- a X + (b A + c A A) X;   out = scale * X.
+ * Each step maps the singular values s of X to a s + b s^3 + c s^5 and leaves its singular vectors. G: DEVICE, `batch` matrices of
+ * rows x cols, element (i, r, t) at i * stride + r * ld + t; out: DEVICE, of the same type, with stride_out and ld_out; the two
+ * must not overlap unless they are the same memory with the same strides. coefficients: HOST, 3 * steps floats (a, b, c of each
+ * step). batch >= 0, 1 <= rows, cols <= 32768, 1 <= steps <= 32, eps >= 0, ld >= cols, batched matrices disjoint. SAGE_ERR_ARG also
+ * for coefficients under which singular values in [0, 1] pass 2^10 on the way. A zero matrix gives zero.
+ * X, A and the polynomial are kept as two fp16 parts, scaled by the bound U of the singular values that the coefficients give (1 before the
+ * first step): 22 bits and more of entries above 2^-17 U, 2^-39 U of smaller ones. Products of parts are summed in fp32, the norm in
+ * fp64. So the result is good to fp32 rounding of the products, for both types, unless eps is so large beside the norm that X
+ * itself is below these.
+ * work: DEVICE, sage_orthogonalize_work's number of bytes, 256-byte aligned; calls that overlap in time need their own. Its
+ * contents do not matter before and after. Asynchronous on hip_stream; allocates nothing and may be captured in a graph.
+ */
+int sage_orthogonalize_work(sage_dtype dtype, int64_t batch, int64_t rows, int64_t cols, size_t* bytes);
+int sage_orthogonalize(const void* G, sage_dtype dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
+                       const float* coefficients, int steps, float eps, float scale, void* out, int64_t ld_out,
+                       int64_t stride_out, void* work, size_t work_bytes, void* hip_stream);
+
 /*
  * Stage probes for tests: run the Gram of the current buffer (C_out: DEVICE, n_pad*n_pad doubles, row-major,
  * n_pad returned in *n_pad) and, if eig != 0, the eigensolve of it (Y_out: DEVICE n_pad*n_pad doubles

@@ -22,7 +22,7 @@ EXPORTS = (
     "sage_destroy", "sage_sync", "sage_set_projection_mode", "sage_fd_sketch_export", "sage_basis_export", "sage_set_basis", "sage_scores",
     "sage_scores_export", "sage_zhat_export", "sage_stats", "sage_topm", "sage_topm_static", "sage_probe_gram_eig", "sage_probe_eig_matrix",
     "sage_profile_enable", "sage_copy_probe", "sage_set_debug_checks", "sage_debug_fail_launch", "sage_debug_impatient_solves", "sage_set_sweep_policy",
-    "sage_profile_read", "sage_strerror",
+    "sage_profile_read", "sage_strerror", "sage_sample", "sage_logit_error", "sage_orthogonalize_work", "sage_orthogonalize",
 )
 
 
@@ -31,6 +31,12 @@ class SageStats(C.Structure):
                 ("sum_delta", C.c_double), ("frob2", C.c_double), ("last_delta", C.c_double),
                 ("last_sweeps", C.c_int), ("fill", C.c_int), ("n_unconverged", C.c_int64),
                 ("last_offdiag", C.c_double)]
+
+
+class SageSampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("temperature_rows", C.c_void_p), ("top_k_rows", C.c_void_p), ("top_p_rows", C.c_void_p),
+                ("min_p_rows", C.c_void_p)]
 
 
 class SageError(RuntimeError):
@@ -118,6 +124,11 @@ def lib():
     L.sage_profile_enable.argtypes = [vp, i32]
     L.sage_profile_read.argtypes = [vp, i32, C.POINTER(dbl), C.POINTER(i64)]
     L.sage_strerror.argtypes = [i32]
+    L.sage_sample.argtypes = [vp, i32, i64, i64, i64, vp, C.POINTER(SageSampling), vp, vp, vp]
+    L.sage_logit_error.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, i32, i64, vp, vp]
+    L.sage_orthogonalize_work.argtypes = [i32, i64, i64, i64, C.POINTER(C.c_size_t)]
+    L.sage_orthogonalize.argtypes = [vp, i32, i64, i64, i64, i64, i64, C.POINTER(C.c_float), i32, C.c_float, C.c_float, vp, i64, i64,
+                                     vp, C.c_size_t, vp]
     L.sage_strerror.restype = C.c_char_p
     for name in EXPORTS:
         if name not in ("sage_destroy", "sage_strerror"):
@@ -392,3 +403,143 @@ def topm_static(alpha, m, out):
     assert out.is_cuda and out.dtype == torch.int64 and out.is_contiguous() and out.numel() >= m
     _check(lib().sage_topm_static(_ptr(alpha), alpha.numel(), m, _ptr(out), _stream(torch)), "sage_topm_static")
     return out[:m]
+
+
+MAX_CLASSES = 1048576  # SAGE_MAX_CLASSES
+
+
+def _need(ok, what):
+    """Arguments that the library cannot look into (types, devices, shapes) are refused like those that it refuses."""
+    if not ok:
+        raise SageError(SAGE_ERR_ARG, what)
+
+
+def _code(torch, dtype, what):
+    _need(dtype in (torch.float32, torch.bfloat16), what)
+    return SAGE_BF16 if dtype == torch.bfloat16 else SAGE_F32
+
+
+def _here(torch, t, what, dtype=None, shape=None):
+    """t is a tensor on the current device (of a type and shape, contiguous, if they are given)."""
+    _need(torch.is_tensor(t) and t.is_cuda and t.device.index == torch.cuda.current_device(), what)
+    _need(dtype is None or t.dtype == dtype, what)
+    _need(shape is None or (tuple(t.shape) == tuple(shape) and t.is_contiguous()), what)
+    return t
+
+
+def _logits(torch, logits, what):
+    """rows x classes with classes next to each other -> (type code, rows, classes, stride of the rows)"""
+    _here(torch, logits, what)
+    _need(logits.dim() == 2 and logits.shape[1] >= 1, what)
+    rows, classes = logits.shape
+    _need(classes == 1 or logits.stride(1) == 1, what)
+    ld = logits.stride(0) if rows > 1 else classes
+    _need(ld >= classes, what)
+    return _code(torch, logits.dtype, what), rows, classes, ld
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """A label for every row of logits (rows x classes, float32 or bfloat16, rows at any stride), drawn with the random numbers u
+    (float32, one per row, in [0, 1)): int32 labels, and float32 log-probabilities under the distribution drawn from.
+
+    temperature, top_k, top_p, min_p: a number for all rows, or a device tensor with one per row (top_k int32, the others float32);
+    see sage_sample in include/sage.h for the order in which they act, ties, and rows without a distribution (label -1).
+    """
+    import torch
+
+    what = "sage_sample"
+    code, rows, classes, ld = _logits(torch, logits, what)
+    _here(torch, u, what, torch.float32, (rows,))
+    how = SageSampling()
+    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                               ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if torch.is_tensor(value):
+            setattr(how, name + "_rows", _here(torch, value, what, dtype, (rows,)).data_ptr())
+        elif name == "top_k":
+            how.top_k = max(0, min(int(value), 0x7FFFFFFF))
+        else:
+            setattr(how, name, float(value))
+    labels = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    logp = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    _check(lib().sage_sample(_ptr(logits), code, rows, classes, ld, _ptr(u), C.byref(how), _ptr(labels), _ptr(logp), _stream(torch)), what)
+    return labels, logp
+
+
+def logit_error(logits, labels, weights=None, out=None, dtype=None):
+    """Cross-entropy of the rows of logits (as for sample) with their labels (int32, below 0: none) and its gradient: (E, loss), E being
+    weights * (softmax(logits) - onehot(labels)), rows x classes, as fd_update_outer and score_outer take it; loss float32, one per row.
+
+    out: where E goes, rows x classes at any stride of the rows, possibly the logits themselves; dtype: E's type if there is no
+    out (the logits' otherwise).
+    """
+    import torch
+
+    what = "sage_logit_error"
+    code, rows, classes, ld = _logits(torch, logits, what)
+    _here(torch, labels, what, torch.int32, (rows,))
+    if weights is not None:
+        _here(torch, weights, what, torch.float32, (rows,))
+    if out is None:
+        out = torch.empty((rows, classes), dtype=logits.dtype if dtype is None else dtype, device=logits.device)
+    e_code, e_rows, e_classes, e_ld = _logits(torch, out, what)
+    _need((e_rows, e_classes) == (rows, classes) and (dtype is None or out.dtype == dtype), what)
+    loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    _check(lib().sage_logit_error(_ptr(logits), code, rows, classes, ld, _ptr(labels), _ptr(weights), _ptr(out), e_code, e_ld, _ptr(loss),
+                                  _stream(torch)), what)
+    return out, loss
+
+
+MUON = (3.4445, -4.7750, 2.0315)  # of a step of orthogonalize: singular values end between about 0.7 and 1.2
+
+
+def _matrices(torch, G, what):
+    """A matrix, or several, with rows or columns next to each other -> (batch, rows, cols, ld, stride, transposed)"""
+    _here(torch, G, what)
+    _need(G.dim() in (2, 3) and G.shape[-2] >= 1 and G.shape[-1] >= 1, what)
+    rows, cols = G.shape[-2:]
+    batch = G.shape[0] if G.dim() == 3 else 1
+    sr, sc = G.stride(-2), G.stride(-1)
+    by_row = (cols == 1 or sc == 1) and (rows == 1 or sr >= cols)
+    by_col = (rows == 1 or sr == 1) and (cols == 1 or sc >= rows)
+    _need(by_row or by_col, what)
+    if not by_row:
+        rows, cols, sr, sc = cols, rows, sc, sr
+    ld = sr if rows > 1 else cols
+    stride = G.stride(0) if batch > 1 else (rows - 1) * ld + cols
+    _need(ld >= cols and stride >= (rows - 1) * ld + cols, what)
+    return batch, rows, cols, ld, stride, not by_row
+
+
+def orthogonalize(G, steps=5, coefficients=MUON, eps=1e-7, scale=1.0, out=None):
+    """Matrices (rows x cols, or batch x rows x cols, float32 or bfloat16) made orthogonal by `steps` Newton-Schulz products: each step
+    maps the singular values s to a s + b s^3 + c s^5, beginning with those of G / (||G||_F + eps); the result times scale.
+
+    G: rows or columns next to each other, at any stride (a transposed view too). coefficients: (a, b, c) for every step, or one
+    such triple for each. out: where the result goes, in the same order of rows and columns as G; possibly G itself.
+    """
+    import torch
+
+    what = "sage_orthogonalize"
+    steps = int(steps)
+    triples = list(coefficients)
+    if triples and not hasattr(triples[0], "__len__"):
+        triples = [triples] * max(steps, 0)
+    _need(len(triples) == steps and all(len(t) == 3 for t in triples), what)
+    flat = [float(v) for t in triples for v in t]
+    batch, rows, cols, ld, stride, turned = _matrices(torch, G, what)
+    code = _code(torch, G.dtype, what)
+    if out is None:
+        out = torch.empty(G.shape[:-2] + (rows, cols), dtype=G.dtype, device=G.device)
+        out = out.transpose(-1, -2) if turned else out
+    _need(out.dtype == G.dtype and out.shape == G.shape, what)
+    o_batch, o_rows, o_cols, o_ld, o_stride, o_turned = _matrices(torch, out, what)
+    if o_turned != turned and 1 in (rows, cols):  # a single row or column may be called either
+        o_rows, o_cols, o_ld, o_turned = o_cols, o_rows, max(o_ld, o_cols), turned
+    _need(o_turned == turned, what)
+    L = lib()
+    need = C.c_size_t(0)
+    _check(L.sage_orthogonalize_work(code, batch, rows, cols, C.byref(need)), what)
+    work = torch.empty(max(need.value, 1), dtype=torch.uint8, device=G.device)
+    _check(L.sage_orthogonalize(_ptr(G), code, batch, rows, cols, ld, stride, (C.c_float * len(flat))(*flat), steps, float(eps), float(scale),
+                                _ptr(out), o_ld, o_stride, C.c_void_p(work.data_ptr()), need.value, _stream(torch)), what)
+    return out

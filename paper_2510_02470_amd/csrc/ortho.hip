@@ -1,0 +1,484 @@
+// Matrices made orthogonal by Newton-Schulz products: sage_orthogonalize (include/sage.h).
+//
+// With m <= n (a taller matrix is worked on as its transpose) and X = G / (||G||_F + eps), a step is three products:
+//     A = X X^T  (m^2 n multiplications, half of them by symmetry),  P = a I + b A + c A A  (m^3, half),  X <- P X  (m^2 n).
+// It is bound by the matrix cores. A step stretches the small singular values by a, 3.4 with the usual coefficients and 485 in
+// five steps, and with them whatever rounding has put into their directions: factors of one bf16 or fp16 part (2^-9, 2^-12) would be seen
+// in the result. So every entry is kept as the sum of two fp16 parts, hi + lo, and hi hi + hi lo + lo hi are summed in fp32: three
+// products on the fp16 matrix cores for one. Two fp16 parts hold 22 bits and more, as fp32 does, where the low part is a normal
+// number; entries are bounded by the largest singular value, whose bound U is known on the host (it follows from the
+// coefficients), so that scaling by a power of two to 2^15 / U leaves entries of 2^-17 U and above that precision and the rest an error
+// of 2^-40 U. (bf16 parts would need three of them, six products.)
+//
+// Layout: 32 columns of a row are 128 bytes, their 32 hi parts and then their 32 lo parts; rows and columns are padded with zeros to
+// multiples of 128. X is kept row by row for A and column by column for P X: the instructions take both factors along the
+// summed index.
+#include <math.h>
+
+#include <algorithm>
+
+#include "sage_internal.h"
+
+namespace sage {
+namespace {
+
+typedef _Float16 f16;
+typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+typedef f16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int PAD = 128;
+constexpr int KB = 32;  // columns of a block of 128 bytes
+
+// A padded matrix in parts: element (r, k) is p[r * pitch + (k / 32) * 64 + k % 32] + the one 32 further.
+struct Parts {
+    f16* p;
+    int64_t pitch;  // 2 * padded columns
+    int64_t batch;  // from one matrix to the next
+};
+
+__device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
+    hi = (f16)v;
+    lo = (f16)(v - (float)hi);
+}
+
+// ---- X: the norm, and the matrix in parts both ways -------------------------------------------------------------
+
+template <class T>
+__device__ __forceinline__ float widen(T x) {
+    if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)x << 16);
+    else return x;
+}
+template <class T>
+__device__ __forceinline__ T narrow(float x) {
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t u = __float_as_uint(x);
+        if (x != x) return (T)(u >> 16 | 0x40);
+        return (T)((u + 0x7FFF + (u >> 16 & 1)) >> 16);
+    } else {
+        return x;
+    }
+}
+
+constexpr int NORM_THREADS = 256;
+
+// Sums of squares of groups of rows, in fp64: any fp32 matrix has a norm there.
+template <class T>
+__global__ __launch_bounds__(NORM_THREADS) void ortho_norm_kernel(const T* __restrict__ G, int64_t rows, int64_t cols, int64_t ld,
+                                                                  int64_t stride, double* __restrict__ partial, int groups) {
+    __shared__ double part[NORM_THREADS / 64];
+    const int group = blockIdx.x % groups;
+    const int64_t b = blockIdx.x / groups;
+    double s = 0.0;
+    for (int64_t r = group; r < rows; r += groups) {
+        const T* row = G + b * stride + r * ld;
+        for (int64_t t = threadIdx.x; t < cols; t += NORM_THREADS) {
+            const double x = widen(row[t]);
+            s = __builtin_fma(x, x, s);
+        }
+    }
+    for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) partial[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+}
+
+// 64 x 64 tiles of scale * G / (norm + eps), row by row into R and column by column into Q; what is outside of G is zero.
+template <class T>
+__global__ __launch_bounds__(256) void ortho_split_kernel(const T* __restrict__ G, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
+                                                          const double* __restrict__ partial, int groups, double eps, double scale,
+                                                          Parts R, Parts Q, int tiles_r, int tiles_c) {
+    __shared__ float tile[64][65];
+    const int64_t b = blockIdx.x / (tiles_r * tiles_c);
+    const int at = blockIdx.x % (tiles_r * tiles_c);
+    const int64_t r0 = (int64_t)(at / tiles_c) * 64, c0 = (int64_t)(at % tiles_c) * 64;
+    double s = 0.0;
+    for (int i = 0; i < groups; ++i) s += partial[b * groups + i];
+    const double inv = s > 0.0 || s != s ? scale / (sqrt(s) + eps) : 0.0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const T* g = G + b * stride;
+    f16* rp = R.p + b * R.batch + (c0 >> 5) * 64 + (lane >> 5) * 64 + (lane & 31);
+    f16* qp = Q.p + b * Q.batch + (r0 >> 5) * 64 + (lane >> 5) * 64 + (lane & 31);
+    for (int i = wave; i < 64; i += 4) {
+        const int64_t r = r0 + i, c = c0 + lane;
+        const float v = r < rows && c < cols ? (float)((double)widen(g[r * ld + c]) * inv) : 0.f;
+        tile[i][lane] = v;
+        f16 hi, lo;
+        split(v, hi, lo);
+        rp[r * R.pitch] = hi;
+        rp[r * R.pitch + 32] = lo;
+    }
+    __syncthreads();
+    for (int i = wave; i < 64; i += 4) {
+        f16 hi, lo;
+        split(tile[lane][i], hi, lo);
+        qp[(c0 + i) * Q.pitch] = hi;
+        qp[(c0 + i) * Q.pitch + 32] = lo;
+    }
+}
+
+// ---- the products -----------------------------------------------------------------------------------------------
+
+enum { GRAM, POLY, STEP, LAST };
+
+struct Finish {
+    float f;      // of the sum
+    float fa;     // of A's entry (POLY)
+    float diag;   // added on the diagonal (GRAM, POLY)
+    Parts A;      // POLY
+    Parts C;      // the result, row by row
+    Parts Ct;     // STEP: and column by column
+    void* out;    // LAST
+    int64_t ld_out, stride_out, rows, cols;
+    int out16;
+};
+
+// Tile t of a lower triangle: row i, column j <= i.
+__device__ __forceinline__ void triangle(int t, int& i, int& j) {
+    i = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while ((int64_t)i * (i + 1) / 2 > t) --i;
+    while ((int64_t)(i + 1) * (i + 2) / 2 <= t) ++i;
+    j = t - (int)((int64_t)i * (i + 1) / 2);
+}
+
+// C = A B^T of padded matrices in parts, both along the summed index: tiles of 32 WR RB x 32 WC CB, WR x WC waves with RB x CB
+// instruction tiles of 32 x 32 each. Blocks of 32 of the summed index go straight to LDS, one on its way while one is multiplied; a row's
+// eight pieces of 16 bytes are stored in an order turned by the row's number, so that the reads of eight rows meet
+// different banks. (The loads deposit in lane order: it is their addresses that are turned.)
+template <int WR, int WC, int RB, int CB, int MODE>
+__global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin) {
+    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, THREADS = WR * WC * 64;
+    constexpr int STAGE = (TM + TN) * 8;  // pieces of 16 bytes
+    constexpr int LOADS = STAGE / THREADS;
+    static_assert(STAGE % THREADS == 0 && TM * 8 % THREADS == 0, "whole loads");
+    extern __shared__ u32x4 lds[];  // 2 * STAGE
+    constexpr bool SYM = MODE == GRAM || MODE == POLY;
+    const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
+    const int64_t b = blockIdx.x / per;
+    const int at = blockIdx.x % per;
+    int ti, tj;
+    if constexpr (SYM) {
+        triangle(at, ti, tj);
+    } else {
+        ti = at / tiles_c;
+        tj = at % tiles_c;
+    }
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, h = lane >> 5;
+    const int wr = wave / WC, wc = wave % WC;
+
+    const f16* src[LOADS];
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) {
+        const int piece = q * THREADS + tid, row = piece >> 3, turned = (piece & 7) ^ (row & 7);
+        if (q * THREADS < TM * 8) src[q] = A.p + b * A.batch + ((int64_t)ti * TM + row) * A.pitch + turned * 8;
+        else src[q] = B.p + b * B.batch + ((int64_t)tj * TN + row - TM) * B.pitch + turned * 8;
+    }
+    auto stage = [&](int kb, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[q] + (int64_t)kb * 64),
+                                             (__attribute__((address_space(3))) void*)(lds + buf * STAGE + q * THREADS + wave * 64), 16, 0, 0);
+    };
+
+    f32x16 acc[RB][CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+    stage(0, 0);
+    const int arow = wr * 32 * RB + l32, brow = TM + wc * 32 * CB + l32;
+    for (int kb = 0; kb < kblocks; ++kb) {
+        // this block has landed; everyone is done with the buffer of the one before
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (kb + 1 < kblocks) stage(kb + 1, (kb + 1) & 1);
+        const u32x4* st = lds + (kb & 1) * STAGE;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            f16x8 a[RB][2], c[CB][2];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int piece = (4 * p + 2 * s + h) ^ (l32 & 7);
+#pragma unroll
+                for (int i = 0; i < RB; ++i) a[i][p] = __builtin_bit_cast(f16x8, st[(arow + 32 * i) * 8 + piece]);
+#pragma unroll
+                for (int j = 0; j < CB; ++j) c[j][p] = __builtin_bit_cast(f16x8, st[(brow + 32 * j) * 8 + piece]);
+            }
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][1], c[j][0], acc[i][j], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], c[j][1], acc[i][j], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], c[j][0], acc[i][j], 0, 0, 0);
+        }
+    }
+
+    // A lane has four consecutive rows of one column: entries 4 g .. 4 g + 3 are rows 8 g + 4 h + 0 .. 3.
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int64_t r = (int64_t)ti * TM + (wr * RB + i) * 32 + 8 * g + 4 * h;
+                const int64_t c = (int64_t)tj * TN + (wc * CB + j) * 32 + l32;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e] * fin.f;
+                if constexpr (MODE == LAST) {
+                    if (c < fin.cols) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (r + e < fin.rows) {
+                                const int64_t o = b * fin.stride_out + (r + e) * fin.ld_out + c;
+                                if (fin.out16) ((uint16_t*)fin.out)[o] = narrow<uint16_t>(v[e]);
+                                else ((float*)fin.out)[o] = v[e];
+                            }
+                    }
+                } else {
+                    const int64_t at_c = (c >> 5) * 64 + (c & 31), at_r = (r >> 5) * 64 + (r & 31);
+                    if constexpr (MODE == POLY) {
+                        const f16* ap = fin.A.p + b * fin.A.batch + r * fin.A.pitch + at_c;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            v[e] = fmaf(fin.fa, (float)ap[e * fin.A.pitch] + (float)ap[e * fin.A.pitch + 32], v[e]);
+                    }
+                    if constexpr (SYM) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (r + e == c) v[e] += fin.diag;
+                    }
+                    f16x4 hi, lo;
+                    f16* cp = fin.C.p + b * fin.C.batch + r * fin.C.pitch + at_c;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        f16 x, y;
+                        split(v[e], x, y);
+                        hi[e] = x;
+                        lo[e] = y;
+                        cp[e * fin.C.pitch] = x;
+                        cp[e * fin.C.pitch + 32] = y;
+                    }
+                    // the same values the other way round; a diagonal tile has its own mirror image in it
+                    if (MODE == STEP || ti != tj) {
+                        const Parts& t = MODE == STEP ? fin.Ct : fin.C;
+                        f16* tp = t.p + b * t.batch + c * t.pitch + at_r;
+                        *(f16x4*)tp = hi;
+                        *(f16x4*)(tp + 32) = lo;
+                    }
+                }
+            }
+}
+
+// ---- the plan ---------------------------------------------------------------------------------------------------
+
+constexpr int MAX_SIDE = 32768, MAX_STEPS = 32;
+constexpr int64_t WORK_LIMIT = 1ll << 30;  // batches are taken in chunks that need no more, or one matrix at a time
+
+struct Plan {
+    int64_t m, n, M, N;  // the sides, smaller first, and padded
+    int groups;          // of rows, for the norm
+    int64_t x, a;        // halves of X (either way) and of A
+    int64_t per;         // bytes of one matrix
+    int64_t chunk;       // matrices at a time
+};
+
+int64_t padded(int64_t v) { return (v + PAD - 1) / PAD * PAD; }
+int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
+
+Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
+    Plan p;
+    p.m = std::min(rows, cols);
+    p.n = std::max(rows, cols);
+    p.M = padded(p.m);
+    p.N = padded(p.n);
+    p.groups = (int)std::min<int64_t>(rows, std::max<int64_t>(1, std::min<int64_t>(256, rows * cols / 4096)));
+    p.x = 2 * p.M * p.N;
+    p.a = 2 * p.M * p.M;
+    p.per = (3 * p.x + 2 * p.a) * 2 + align256(8 * p.groups);
+    p.chunk = std::max<int64_t>(1, std::min(batch, WORK_LIMIT / p.per));
+    return p;
+}
+
+// max |a s + b s^3 + c s^5| (odd) or max |a + b l + c l^2| over [0, top]: at the ends or where the derivative vanishes
+double bound_of(double a, double b, double c, double top, bool odd) {
+    auto at = [&](double l) { return fabs((odd ? sqrt(l) : 1.0) * (a + l * (b + l * c))); };  // l = s^2
+    const double end = odd ? top * top : top;
+    double r = std::max(at(0.0), at(end));
+    // roots in l of a + 3 b l + 5 c l^2, or of b + 2 c l
+    const double A = odd ? 5 * c : 0.0, B = odd ? 3 * b : 2 * c, C = odd ? a : b;
+    double root[2] = {-1.0, -1.0};
+    if (A != 0.0) {
+        const double d = B * B - 4 * A * C;
+        if (d >= 0.0) {
+            root[0] = (-B + sqrt(d)) / (2 * A);
+            root[1] = (-B - sqrt(d)) / (2 * A);
+        }
+    } else if (B != 0.0) {
+        root[0] = -C / B;
+    }
+    for (double l : root)
+        if (l > 0.0 && l < end) r = std::max(r, at(l));
+    return r;
+}
+
+// the power of two that takes values up to `top` to 2^14 .. 2^15
+double scale_for(double top) {
+    int e;
+    frexp(std::max(top, 0x1p-12), &e);
+    return ldexp(1.0, 15 - e);
+}
+
+template <int MODE>
+hipError_t product(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, hipStream_t st) {
+    constexpr int WR = 2, WC = 2, RB = 2, CB = 2;
+    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, BYTES = 2 * (TM + TN) * 128;
+    const auto kernel = ortho_product_kernel<WR, WC, RB, CB, MODE>;
+    if (hipError_t e = ensure_dynamic_lds((const void*)kernel, BYTES); e != hipSuccess) return e;
+    const int tr = (int)(rows / TM), tc = (int)(cols / TN);
+    const int64_t per = MODE == GRAM || MODE == POLY ? (int64_t)tr * (tr + 1) / 2 : (int64_t)tr * tc;
+    kernel<<<dim3((unsigned)(per * batch)), WR * WC * 64, BYTES, st>>>(A, B, (int)(k / KB), tr, tc, fin);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride, const float* coef, int steps,
+               double eps, double scale, T* out, int64_t ld_out, int64_t stride_out, char* work, hipStream_t st) {
+    const bool tall = rows > cols;
+    f16* w = (f16*)work;
+    const int64_t c = p.chunk;
+    Parts X{w, 2 * p.N, p.x}, Xt[2] = {{w + c * p.x, 2 * p.M, p.x}, {w + 2 * c * p.x, 2 * p.M, p.x}};
+    w += 3 * c * p.x;
+    const Parts A{w, 2 * p.M, p.a}, P{w + c * p.a, 2 * p.M, p.a};
+    double* partial = (double*)(w + 2 * c * p.a);
+
+    ortho_norm_kernel<T><<<dim3((unsigned)(p.groups * batch)), NORM_THREADS, 0, st>>>(G, rows, cols, ld, stride, partial, p.groups);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    double U = 1.0 + 0x1p-10;  // of the singular values
+    double sx = scale_for(U);
+    const int tr = (int)((tall ? p.N : p.M) / 64), tc = (int)((tall ? p.M : p.N) / 64);
+    ortho_split_kernel<T><<<dim3((unsigned)((int64_t)tr * tc * batch)), 256, 0, st>>>(G, rows, cols, ld, stride, partial, p.groups, eps, sx,
+                                                                                      tall ? Xt[0] : X, tall ? X : Xt[0], tr, tc);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    for (int s = 0; s < steps; ++s) {
+        const double ca = coef[3 * s], cb = coef[3 * s + 1], cc = coef[3 * s + 2];
+        const double next = bound_of(ca, cb, cc, U, true) * (1.0 + 0x1p-10);
+        const double sa = scale_for(U * U), sp = scale_for(bound_of(ca, cb, cc, U * U, false)), sn = scale_for(next);
+        Finish f{};
+        if (cc != 0.0) {
+            f.f = (float)(sa / (sx * sx));
+            f.C = A;
+            if (hipError_t e = product<GRAM>(X, X, p.M, p.M, p.N, batch, f, st); e != hipSuccess) return e;
+            f.f = (float)(cc * sp / (sa * sa));
+            f.fa = (float)(cb * sp / sa);
+            f.diag = (float)(ca * sp);
+            f.A = A;
+            f.C = P;
+            if (hipError_t e = product<POLY>(A, A, p.M, p.M, p.M, batch, f, st); e != hipSuccess) return e;
+        } else {
+            f.f = (float)(cb * sp / (sx * sx));
+            f.diag = (float)(ca * sp);
+            f.C = P;
+            if (hipError_t e = product<GRAM>(X, X, p.M, p.M, p.N, batch, f, st); e != hipSuccess) return e;
+        }
+        const Parts& xt = Xt[s & 1];
+        if (s + 1 < steps) {
+            f.f = (float)(sn / (sp * sx));
+            f.C = X;
+            f.Ct = Xt[(s + 1) & 1];
+            if (hipError_t e = product<STEP>(P, xt, p.M, p.N, p.M, batch, f, st); e != hipSuccess) return e;
+        } else {
+            f.f = (float)(scale / (sp * sx));
+            f.out = out;
+            f.ld_out = ld_out;
+            f.stride_out = stride_out;
+            f.rows = rows;
+            f.cols = cols;
+            f.out16 = sizeof(T) == 2;
+            const hipError_t e = tall ? product<LAST>(xt, P, p.N, p.M, p.M, batch, f, st) : product<LAST>(P, xt, p.M, p.N, p.M, batch, f, st);
+            if (e != hipSuccess) return e;
+        }
+        U = next;
+        sx = sn;
+    }
+    return hipSuccess;
+}
+
+bool sizes_ok(int dtype, int64_t batch, int64_t rows, int64_t cols) {
+    return (dtype == SAGE_F32 || dtype == SAGE_BF16) && batch >= 0 && batch <= (1ll << 31) && rows >= 1 && rows <= MAX_SIDE && cols >= 1 &&
+           cols <= MAX_SIDE;
+}
+
+// rows of `cols` every ld, matrices every stride, none reaching into another, all offsets in 62 bits
+bool layout_ok(const void* p, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride) {
+    if (!p || (uintptr_t)p % (dtype == SAGE_BF16 ? 2 : 4) || ld < cols || ld > (1ll << 40)) return false;
+    const int64_t one = (rows - 1) * ld + cols;
+    return batch <= 1 || (stride >= one && stride <= (1ll << 59) / batch);
+}
+
+}  // namespace
+}  // namespace sage
+
+extern "C" int sage_orthogonalize_work(sage_dtype dtype, int64_t batch, int64_t rows, int64_t cols, size_t* bytes) {
+    if (!bytes || !sage::sizes_ok(dtype, batch, rows, cols)) return SAGE_ERR_ARG;
+    const sage::Plan p = sage::plan_of(batch, rows, cols);
+    *bytes = batch ? (size_t)(p.per * p.chunk) : 0;
+    return SAGE_OK;
+}
+
+extern "C" int sage_orthogonalize(const void* G, sage_dtype dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
+                                  const float* coefficients, int steps, float eps, float scale, void* out, int64_t ld_out,
+                                  int64_t stride_out, void* work, size_t work_bytes, void* hip_stream) {
+    using namespace sage;
+    if (!sizes_ok(dtype, batch, rows, cols) || !coefficients || steps < 1 || steps > MAX_STEPS || !(eps >= 0.f) || !(eps < INFINITY) ||
+        !(fabsf(scale) < INFINITY))
+        return SAGE_ERR_ARG;
+    double U = 1.0 + 0x1p-10;
+    for (int s = 0; s < steps; ++s) {
+        const float* c = coefficients + 3 * s;
+        for (int i = 0; i < 3; ++i)
+            if (!(fabsf(c[i]) <= 1024.f)) return SAGE_ERR_ARG;
+        U = bound_of(c[0], c[1], c[2], U, true) * (1.0 + 0x1p-10);
+        if (!(U <= 1024.0)) return SAGE_ERR_ARG;
+    }
+    if (batch == 0) return SAGE_OK;
+    if (!layout_ok(G, dtype, batch, rows, cols, ld, stride) || !layout_ok(out, dtype, batch, rows, cols, ld_out, stride_out)) return SAGE_ERR_ARG;
+    const int64_t es = dtype == SAGE_BF16 ? 2 : 4;
+    if (!(G == out && ld == ld_out && (batch == 1 || stride == stride_out))) {
+        const uintptr_t g0 = (uintptr_t)G, o0 = (uintptr_t)out;
+        const uintptr_t g1 = g0 + es * ((batch > 1 ? (batch - 1) * stride : 0) + (rows - 1) * ld + cols);
+        const uintptr_t o1 = o0 + es * ((batch > 1 ? (batch - 1) * stride_out : 0) + (rows - 1) * ld_out + cols);
+        if (g0 < o1 && o0 < g1) return SAGE_ERR_ARG;
+    }
+    const Plan p = plan_of(batch, rows, cols);
+    if (!work || (uintptr_t)work % 256 || work_bytes < (size_t)(p.per * p.chunk)) return SAGE_ERR_ARG;
+    for (int64_t b = 0; b < batch; b += p.chunk) {
+        const int64_t n = std::min(p.chunk, batch - b);
+        const hipError_t e =
+            dtype == SAGE_F32
+                ? run<float>(p, (const float*)G + b * stride, n, rows, cols, ld, stride, coefficients, steps, eps, scale,
+                             (float*)out + b * stride_out, ld_out, stride_out, (char*)work, (hipStream_t)hip_stream)
+                : run<uint16_t>(p, (const uint16_t*)G + b * stride, n, rows, cols, ld, stride, coefficients, steps, eps, scale,
+                                (uint16_t*)out + b * stride_out, ld_out, stride_out, (char*)work, (hipStream_t)hip_stream);
+        if (e != hipSuccess) {
+            (void)hipGetLastError();
+            return SAGE_ERR_HIP;
+        }
+    }
+    return SAGE_OK;
+}

@@ -370,4 +370,9 @@ CbWork cb_work_layout(void* base, int C, int64_t N);
 hipError_t launch_cb_select(const float* zhat, const int* labels, int64_t N, int k, int C, double keep, int rule,
                             float* alpha, int64_t cap, int64_t* out_idx, uint32_t* report, const CbWork& w, hipStream_t st);
 
+// Rows of logits (sample.hip, logit_error.hip): type, sizes, stride and alignment are ones the kernels take.
+constexpr int64_t LOGIT_LAUNCH_ROWS = 1 << 20;  // a launch has fewer than 2^32 threads
+bool logit_rows_ok(const void* p, int dtype, int64_t rows, int64_t C, int64_t ld);
+bool rows_overlap(const void* a, int da, int64_t lda, const void* b, int db, int64_t ldb, int64_t rows, int64_t C);
+
 }  // namespace sage
