@@ -9,45 +9,61 @@
 
 #include "logit_rows.h"
 #include "sage_internal.h"
+#include "wave_ops.h"
 
 namespace sage {
 namespace {
 
 // rint(2^42 e^x) for x <= 0: e^x = 2^n e^r with |r| <= ln 2 / 2, and e^r = 1 + r q(r), q of degree 9 through the Chebyshev points
-// (relative error 2^-50; q computed for this with rational numbers). Exactly 2^42 at 0.
-__device__ __forceinline__ uint64_t weight_of(double x) {
-    if (!(x >= -30.0)) return 0;  // (2^42 e^-30 < 1/2)
-    constexpr double ROUND = 6755399441055744.0;  // 1.5 * 2^52: added and taken off again it rounds to a whole number
+// (relative error 2^-50; q computed for this with rational numbers). Exactly 2^42 at 0; 0 below -30, and for NaN (-inf at an infinite
+// temperature). weight_bits is the weight and the bits of ROUND, which a sum takes off once.
+constexpr double ROUND = 6755399441055744.0;  // 1.5 * 2^52: added and taken off again it rounds to a whole number
+constexpr uint64_t ROUND_BITS = 0x4338000000000000ull;
+__device__ __forceinline__ double fma_s(double a, double b, double c) {  // c in scalar registers (the compiler copies it to vector ones)
+    double d;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "s"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t weight_bits(double x) {
+    x = fmax(x, -31.0);  // 2^42 e^-31 rounds to 0
     const double t = __builtin_fma(x, 1.4426950408889634, ROUND);
     const double n = t - ROUND;
     const double r = __builtin_fma(n, -0.6931471805599453, x);
-    double q = 0x1.289185613a3d6p-22;
-    q = __builtin_fma(q, r, 0x1.72e1150d0c9b6p-19);
-    q = __builtin_fma(q, r, 0x1.a019b90d2ae7ap-16);
-    q = __builtin_fma(q, r, 0x1.a01994bd214e7p-13);
-    q = __builtin_fma(q, r, 0x1.6c16c1788bd90p-10);
-    q = __builtin_fma(q, r, 0x1.11111123c1f47p-7);
-    q = __builtin_fma(q, r, 0x1.5555555553d63p-5);
-    q = __builtin_fma(q, r, 0x1.5555555550d79p-3);
-    q = __builtin_fma(q, r, 0x1.0000000000001p-1);
-    q = __builtin_fma(q, r, 0x1.0000000000006p+0);
+    double q = fma_s(0x1.289185613a3d6p-22, r, 0x1.72e1150d0c9b6p-19);
+    q = fma_s(q, r, 0x1.a019b90d2ae7ap-16);
+    q = fma_s(q, r, 0x1.a01994bd214e7p-13);
+    q = fma_s(q, r, 0x1.6c16c1788bd90p-10);
+    q = fma_s(q, r, 0x1.11111123c1f47p-7);
+    q = fma_s(q, r, 0x1.5555555553d63p-5);
+    q = fma_s(q, r, 0x1.5555555550d79p-3);
+    q = fma_s(q, r, 0x1.0000000000001p-1);
+    q = fma_s(q, r, 0x1.0000000000006p+0);
     const double p = __builtin_fma(q, r, 1.0);
-    const int e = (int)__double_as_longlong(t) + 42;  // n + 42 >= -1
-    const double w = __longlong_as_double(__double_as_longlong(p) + ((int64_t)e << 52));
-    return (uint64_t)(__double_as_longlong(w + ROUND) - __double_as_longlong(ROUND));
+    const uint64_t pb = (uint64_t)__double_as_longlong(p);
+    const uint32_t hi = (uint32_t)(pb >> 32) + (((uint32_t)__double_as_longlong(t) + 42u) << 20);  // times 2^(n + 42), n >= -45
+    const double w = __longlong_as_double((long long)((uint64_t)hi << 32 | (uint32_t)pb));
+    return (uint64_t)__double_as_longlong(w + ROUND);
 }
+__device__ __forceinline__ uint64_t weight_of(double x) { return weight_bits(x) - ROUND_BITS; }
 
 // Floats in their order as unsigned numbers; both zeros are one.
 __device__ __forceinline__ uint32_t key_of(float z) {
     const uint32_t u = __float_as_uint(z + 0.f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-// The classes kept so far: those above a key, and of those at it the ones before an index.
+__device__ __forceinline__ float value_of(uint32_t key) {
+    return __uint_as_float(key ^ (key >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+}
+
+// The classes kept so far: those above a value, and of those at it the ones before a place.
 struct Cut {
-    uint32_t key;
-    int index;
-    __device__ bool keeps(uint32_t k, int j) const { return k > key || (k == key && j < index); }
+    float value;
+    int place;
+    __device__ __forceinline__ bool keeps(float x, int j) const { return (x > value) | ((x == value) & (j < place)); }  // (| and &: no branches)
 };
+__device__ __forceinline__ Cut cut_after(uint64_t listed) {  // the last that is kept, as listed
+    return Cut{value_of((uint32_t)(listed >> 32)), (int)~(uint32_t)listed + 1};
+}
 
 // What the THREADS threads of a row share.
 template <int THREADS>
@@ -55,28 +71,34 @@ struct Shared {
     static constexpr int W = THREADS / 64;
     static constexpr int BITS = THREADS == 64 ? 8 : THREADS == 256 ? 10 : 11, BINS = 1 << BITS;  // of a histogram
     static constexpr int LIST = THREADS == 64 ? 128 : THREADS == 256 ? 512 : 1024;  // classes that are put in order one by one
-    static constexpr int SEGS = THREADS == 1024 ? SAGE_MAX_CLASSES / 256 : 16 * W;  // pieces of 64 vectors of the longest row
-    uint64_t hist[BINS > SEGS ? BINS : SEGS];  // a histogram, or the sums of segments
+    static constexpr int SEGS = THREADS >= 512 ? SAGE_MAX_CLASSES / 1024 : W;  // pieces of 64 * U vectors of the longest row
+    uint64_t hist[BINS];  // a histogram (of counts, weights, or approximate weights)
+    uint64_t seg[SEGS];   // sums of segments
     uint64_t part[W];
     float fpart[2 * W];
-    uint64_t lkey[LIST];  // key and place of a listed class, one number in their common order; and its weight
-    uint64_t lw[LIST];
+    uint64_t lkey[LIST], sorted[LIST];  // of listed classes key and place, one number in their common order
+    uint64_t lw[LIST], sw[LIST];        // and weight
     uint64_t found[2];
     unsigned listed;
     uint64_t answer;
 };
 
-// A row as THREADS threads see it: vector i of a thread holds elements (i THREADS + thread) VL .. + VL - 1, those behind the row's
-// end being -inf. STAGED: kept in LDS by load(), else read again for every pass (one vector on its way while one is worked on).
+__device__ __forceinline__ uint64_t mask_of(bool b) { return b ? ~0ull : 0ull; }
+
+constexpr int U = 4;  // vectors of a thread that are read together
+
+// A row as THREADS threads see it. A segment is 64 * U vectors, of which lane l of a wave has vectors l, 64 + l, ..; waves take
+// segments in turn. Elements behind the row's end are -inf. STAGED: the first pass leaves the row in LDS, else it is read again by
+// every pass (one segment on its way while one is worked on).
 template <class T, int THREADS, bool STAGED>
 struct Row {
-    static constexpr int VL = RowType<T>::VL;
+    static constexpr int VL = RowType<T>::VL, W = THREADS / 64;
     static constexpr uint32_t NONE = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
     const T* z;
-    int n, tid, count;  // count: vectors of a thread
-    u32x4* lds;         // count * THREADS
+    int n, tid, count;  // count: segments of a wave
+    u32x4* lds;         // count * THREADS * U
 
-    __device__ u32x4 fetch(int e0) const {
+    __device__ __forceinline__ u32x4 fetch(int e0) const {
         if (e0 + VL <= n) return load16(z + e0);
         u32x4 v = {NONE, NONE, NONE, NONE};
         if (e0 < n) {
@@ -92,184 +114,307 @@ struct Row {
         }
         return v;
     }
-    // f(i, first element, vector), in the order of i; first: the pass that reads the row
+    __device__ __forceinline__ int place(int i, int u) const { return (((i * W + (tid >> 6)) * U + u) * 64 + (tid & 63)) * VL; }  // first element
+    __device__ int segment_of(int j) const { return j / (64 * U * VL); }
+    __device__ __forceinline__ void fetch_segment(int i, u32x4* v) const {
+        if (((i * W + (tid >> 6)) + 1) * (U * 64 * VL) <= n) {  // (the same for the whole wave)
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load16(z + place(i, u));
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = fetch(place(i, u));
+        }
+    }
+    // f(segment of the wave, vectors); first: the pass that reads the row
     template <bool FIRST = false, class F>
     __device__ __forceinline__ void visit(F f) const {
         if constexpr (STAGED && !FIRST) {
 #pragma unroll 1
-            for (int i = 0; i < count; ++i) f(i, (i * THREADS + tid) * VL, lds[i * THREADS + tid]);
+            for (int i = 0; i < count; ++i) {
+                u32x4 v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = lds[(i * U + u) * THREADS + tid];
+                f(i, v);
+            }
         } else {
-            u32x4 v = fetch(tid * VL);
+            u32x4 v[U];
+            fetch_segment(0, v);
 #pragma unroll 1
             for (int i = 0; i < count; ++i) {
-                const u32x4 next = fetch(i + 1 < count ? ((i + 1) * THREADS + tid) * VL : n);
-                if constexpr (STAGED) lds[i * THREADS + tid] = v;
-                f(i, (i * THREADS + tid) * VL, v);
-                v = next;
+                u32x4 next[U];
+                if (i + 1 < count) fetch_segment(i + 1, next);
+                if constexpr (STAGED) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) lds[(i * U + u) * THREADS + tid] = v[u];
+                }
+                f(i, v);
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = next[u];
             }
         }
     }
     // f(value, element) for each element
     template <bool FIRST = false, class F>
     __device__ __forceinline__ void each(F f) const {
-        visit<FIRST>([&](int, int e0, const u32x4& v) __attribute__((always_inline)) {
+        visit<FIRST>([&](int i, const u32x4* v) __attribute__((always_inline)) {
 #pragma unroll
-            for (int k = 0; k < VL; ++k) f(RowType<T>::at(v, k), e0 + k);
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int k = 0; k < VL; ++k) {
+                    if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);  // (more of them mixed would need more registers than there are)
+                    f(RowType<T>::at(v[u], k), place(i, u) + k);
+                }
+            }
         });
     }
 };
 
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_move_u64(uint64_t v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)v, CTRL, 0xF, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(v >> 32), CTRL, 0xF, 0xF, false);
+    return (uint64_t)hi << 32 | lo;
 }
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v, int lane) {  // sums up to and with each lane
+template <int D>
+__device__ __forceinline__ uint64_t add_swapped(uint64_t v) {
+    const unsigned lo = (unsigned)v, hi = (unsigned)(v >> 32);
+    const auto l = D == 16 ? __builtin_amdgcn_permlane16_swap(lo, lo, false, false) : __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+    const auto h = D == 16 ? __builtin_amdgcn_permlane16_swap(hi, hi, false, false) : __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+    return ((uint64_t)h[0] << 32 | l[0]) + ((uint64_t)h[1] << 32 | l[1]);
+}
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {  // the same in every lane
+    v += dpp_move_u64<DPP_XOR1>(v);
+    v += dpp_move_u64<DPP_XOR2>(v);
+    v += dpp_move_u64<DPP_HALF_MIRROR>(v);
+    v += dpp_move_u64<DPP_MIRROR>(v);
+    return add_swapped<32>(add_swapped<16>(v));
+}
+template <class A>
+__device__ __forceinline__ A wave_scan(A v, int lane) {  // sums up to and with each lane
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_up(v, d, 64);
+        const A o = __shfl_up(v, d, 64);
         if (lane >= d) v += o;
     }
     return v;
 }
-
-// The first of `count` sums in LDS up to which they come to more than t: found[0] its number, found[1] the sum of those
-// before it. t < 0 (as an unsigned number, -1): nothing is looked for. Returns the sum of all.
 template <int THREADS>
-__device__ uint64_t find_sum(Shared<THREADS>& S, int count, int tid, uint64_t* t_of_total, const float* u) {
+__device__ __forceinline__ uint64_t group_sum(uint64_t v, Shared<THREADS>& S) {
+    v = wave_sum(v);
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) S.part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = S.part[0];
+#pragma unroll
+        for (int w = 1; w < THREADS / 64; ++w) v += S.part[w];
+    }
+    return v;
+}
+
+// What a random number takes of a sum.
+__device__ __forceinline__ uint64_t share_of(float u, uint64_t total) {
+    const uint64_t t = u > 0.f ? (uint64_t)((double)fminf(u, 1.f) * (double)total) : 0;
+    return t >= total ? total - 1 : t;
+}
+
+// The first of `count` sums in LDS up to which they come to more than t = want(their total): its number, and in S.found the sum of
+// those before it and its own.
+template <int THREADS, class E, class F>
+__device__ __forceinline__ int find_sum(Shared<THREADS>& S, const E* sums, int count, int tid, uint64_t& total, F want) {
     const int per = (count + THREADS - 1) / THREADS;
     uint64_t own = 0;
     for (int i = 0; i < per; ++i)
-        if (tid * per + i < count) own += S.hist[tid * per + i];
+        if (tid * per + i < count) own += sums[tid * per + i];
     const uint64_t incl = wave_scan(own, tid & 63);
-    uint64_t before = incl - own, total = incl;
+    uint64_t before = incl - own;
+    if (tid == 0) S.listed = 0;  // (none, should rounding leave the total out of reach)
     if constexpr (THREADS > 64) {
         if ((tid & 63) == 63) S.part[tid >> 6] = incl;
         __syncthreads();
         total = 0;
+        uint64_t front = 0;
+#pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) {
-            if (w < tid >> 6) before += S.part[w];
+            front = w < tid >> 6 ? front + S.part[w] : front;
             total += S.part[w];
         }
+        before += front;
     } else {
+        __syncthreads();
         total = __shfl(incl, 63, 64);
     }
-    if (u) {  // t from the total: a random number's place in it
-        const float x = *u;
-        uint64_t t = x > 0.f ? (uint64_t)((double)fminf(x, 1.f) * (double)total) : 0;
-        *t_of_total = t >= total ? total - 1 : t;
-    }
-    const uint64_t t = *t_of_total;
+    const uint64_t t = want(total);
     if (before <= t && before + own > t) {
         int i = tid * per;
-        while (before + S.hist[i] <= t) before += S.hist[i++];
-        S.found[0] = (uint64_t)i;
-        S.found[1] = before;
+        while (i < tid * per + per - 1 && i < count - 1 && before + sums[i] <= t) before += sums[i++];
+        S.listed = (unsigned)i;
+        S.found[0] = before;
+        S.found[1] = sums[i];
     }
     __syncthreads();
-    return total;
+    return (int)S.listed;
 }
 
-// The first element up to which f(value, element) sum to more than t, or to more than u's share of their sum, which is returned
-// (the sum in `total`). f is 0 for what lies behind the row's end.
+// With the sums of segments in LDS: the element at which the sum of f (value, element) passes t, the sum of all being total.
 template <class T, int THREADS, bool STAGED, class F>
-__device__ int locate(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t t, const float* u, uint64_t& total, F f) {
+__device__ __forceinline__ int locate_in(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t& total, const float* u, uint64_t t0, F f) {
     constexpr int VL = RowType<T>::VL, W = THREADS / 64;
     const int lane = r.tid & 63, wave = r.tid >> 6;
-    __syncthreads();
-    r.visit([&](int i, int e0, const u32x4& v) __attribute__((always_inline)) {
-        uint64_t own = 0;
-#pragma unroll
-        for (int k = 0; k < VL; ++k) own += f(RowType<T>::at(v, k), e0 + k);
-        const uint64_t s = __any(own != 0) ? wave_sum(own) : 0;
-        if (lane == 0) S.hist[i * W + wave] = s;
-    });
-    __syncthreads();
-    total = find_sum<THREADS>(S, r.count * W, r.tid, &t, u);
-    const int seg = (int)S.found[0];
+    const int seg = find_sum<THREADS>(S, S.seg, r.count * W, r.tid, total,
+                                      [&](uint64_t all) { return u ? share_of(*u, all) : t0; });
+    const uint64_t t = u ? share_of(*u, total) : t0;
     if (wave == seg % W) {
-        const uint64_t base = S.found[1];
-        const int e0 = (seg * 64 + lane) * VL;
-        const u32x4 v = r.fetch(e0);
-        uint64_t w[VL], own = 0;
+        uint64_t before = S.found[0];
+        bool done = false;
+#pragma unroll 1
+        for (int q = 0; q < U; ++q) {
+            const int e0 = ((seg * U + q) * 64 + lane) * VL;
+            const u32x4 v = r.fetch(e0);
+            uint64_t w[VL], own = 0;
 #pragma unroll
-        for (int k = 0; k < VL; ++k) {
-            w[k] = f(RowType<T>::at(v, k), e0 + k);
-            own += w[k];
-        }
-        uint64_t before = base + wave_scan(own, lane) - own;
-        if (before <= t && before + own > t) {
-            int at = 0;
-#pragma unroll
-            for (int k = 0; k < VL - 1; ++k) {  // (no indexing of registers)
-                if (at == k && before + w[k] <= t) {
-                    before += w[k];
-                    ++at;
-                }
+            for (int k = 0; k < VL; ++k) {
+                w[k] = f(RowType<T>::at(v, k), e0 + k);
+                own += w[k];
             }
-            S.answer = (uint64_t)(e0 + at);
+            const uint64_t incl = wave_scan(own, lane);
+            uint64_t mine = before + incl - own;
+            if (!done && mine <= t && mine + own > t) {
+                int at = 0;
+#pragma unroll
+                for (int k = 0; k < VL - 1; ++k) {  // (no indexing of registers)
+                    if (at == k && mine + w[k] <= t) {
+                        mine += w[k];
+                        ++at;
+                    }
+                }
+                S.answer = (uint64_t)(e0 + at);
+            }
+            before += __shfl(incl, 63, 64);
+            done = before > t;
         }
     }
     __syncthreads();
     return (int)S.answer;
 }
 
-// One more histogram of f over the members of a set: bin_of(value) in [0, Shared::BINS), lower bins first in the order, or -1. Finds the bin in
-// which the sum from the front passes t; below: the sum before it (S.found).
-template <class T, int THREADS, bool STAGED, class B, class F>
-__device__ void histogram(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t t, B bin_of, F f) {
+// The same from the row alone. keeps(value, element): f is not 0; bits(value, element): f, and ROUND_BITS if `rounded`, for what is kept.
+template <class T, int THREADS, bool STAGED, class K, class F>
+__device__ __forceinline__ int locate(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t& total, const float* u, uint64_t t0, K keeps, F f) {
+    constexpr int VL = RowType<T>::VL, W = THREADS / 64;
     __syncthreads();
-    for (int i = r.tid; i < S.BINS; i += THREADS) S.hist[i] = 0;
+    r.visit([&](int i, const u32x4* v) __attribute__((always_inline)) {
+        uint64_t own = 0;
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            __builtin_amdgcn_sched_barrier(0);
+            bool any = false;
+#pragma unroll
+            for (int k = 0; k < VL; ++k) any |= keeps(RowType<T>::at(v[q], k), r.place(i, q) + k);
+            if (__any(any)) {
+#pragma unroll
+                for (int k = 0; k < VL; ++k) {
+                    if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                    const float x = RowType<T>::at(v[q], k);
+                    const uint64_t w = f(x, r.place(i, q) + k);
+                    own += w & mask_of(keeps(x, r.place(i, q) + k));
+                }
+            }
+        }
+        const uint64_t s = wave_sum(own);
+        if ((r.tid & 63) == 0) S.seg[i * W + (r.tid >> 6)] = s;
+    });
+    __syncthreads();
+    return locate_in(r, S, total, u, t0, [&](float x, int j) __attribute__((always_inline)) { return f(x, j) & mask_of(keeps(x, j)); });
+}
+
+// The bins of a histogram: equal parts of the distance to the maximum, everything beyond `range` in the last.
+struct Bins {
+    float m, scale, last;
+    __device__ Bins(float m_, float range, int bins) : m(m_), scale((float)(bins - 1) / range), last((float)(bins - 1)) {}
+    __device__ int operator()(float x) const {  // (scale may be infinite: then only the maximum is in bin 0)
+        const float d = m - x;
+        return d > 0.f ? (int)fminf(d * scale, last) : 0;
+    }
+};
+
+// The least value whose bin is at most b (bins fall with the value).
+__device__ __forceinline__ float least_of_bin(const Bins& bins, int b) {
+    uint32_t lo = key_of(-INFINITY), hi = key_of(bins.m);  // hi: in bin 0
+    if (b < 0) return INFINITY;
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (bins(value_of(mid)) <= b) hi = mid;
+        else lo = mid + 1;
+    }
+    return value_of(lo);
+}
+
+template <int THREADS>
+__device__ __forceinline__ void clear_histogram(Shared<THREADS>& S, int tid) {
+    __syncthreads();
+    for (int i = tid; i < S.BINS; i += THREADS) S.hist[i] = 0;
+    __syncthreads();
+}
+
+// Classes whose bin is at most `bin` (or just it), as long as there is room: how many there are.
+template <class T, int THREADS, bool STAGED, class M, class F>
+__device__ __forceinline__ int collect(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, M member, F f) {
+    __syncthreads();
+    if (r.tid == 0) S.listed = 0;
     __syncthreads();
     r.each([&](float x, int j) __attribute__((always_inline)) {
-        const int b = bin_of(x, j);
-        if (b >= 0) {
+        if (member(x, j)) {
             const uint64_t w = f(x, j);
-            if (w) atomicAdd((unsigned long long*)&S.hist[b], (unsigned long long)w);
+            if (w) {
+                const unsigned p = atomicAdd(&S.listed, 1u);
+                if (p < Shared<THREADS>::LIST) {
+                    S.lkey[p] = (uint64_t)key_of(x) << 32 | (uint32_t)~j;  // greater: earlier in the order
+                    S.lw[p] = w;
+                }
+            }
         }
     });
     __syncthreads();
-    find_sum<THREADS>(S, S.BINS, r.tid, &t, nullptr);
+    return (int)S.listed;
 }
 
-// The shortest front part of the order (value descending, place ascending) whose f sum to more than t, as a cut. The sum of all f is more
-// than t. A histogram over the distance to the maximum (equal parts of `range`) leaves one bin; its members are put in order
+// The shortest front part of the order (value descending, place ascending) whose f sum to more than t, as a cut; the sum of all f is more
+// than t. For any f and any row: a histogram over the distance to the maximum leaves one bin; its members are put in order
 // one by one, or, if they are many, told apart by more histograms over their keys first.
 template <class T, int THREADS, bool STAGED, class F>
-__device__ Cut front(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t t, float m, float range, F f) {
-    constexpr float LAST = (float)(Shared<THREADS>::BINS - 1);
+__device__ __forceinline__ Cut front(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t t, const Bins& bins, F f) {
     constexpr int LIST = Shared<THREADS>::LIST, BITS = Shared<THREADS>::BITS;
-    const float scale = LAST / range;  // (may be infinite or 0: bins 0 and, for what is not the maximum, the last)
-    auto bin = [&](float x) __attribute__((always_inline)) {
-        const float d = m - x;
-        return d > 0.f ? (int)fminf(d * scale, LAST) : 0;
-    };
-    histogram(r, S, t, [&](float x, int) __attribute__((always_inline)) { return bin(x); }, f);
-    const int at = (int)S.found[0];
-    uint64_t above = S.found[1];
     uint32_t prefix = 0;
-    int shift = 32;  // keys of the set agree with prefix from this bit on
+    int shift = 33;  // keys of the set agree with prefix from bit `shift` on; 33: the set is everything, 32: a bin of values
+    float from = INFINITY, least = -INFINITY;
+    uint64_t above = 0;
     auto member = [&](float x) __attribute__((always_inline)) {
-        return bin(x) == at && (shift == 32 || key_of(x) >> shift == prefix);
+        return (x < from) & (x >= least) & (shift >= 32 || key_of(x) >> (shift & 31) == prefix);
     };
     for (;;) {
-        __syncthreads();
-        if (r.tid == 0) S.listed = 0;
-        __syncthreads();
+        const int step = shift < BITS ? shift : BITS, low = shift - step;
+        clear_histogram(S, r.tid);
         r.each([&](float x, int j) __attribute__((always_inline)) {
             if (member(x)) {
                 const uint64_t w = f(x, j);
-                if (w) {
-                    const unsigned p = atomicAdd(&S.listed, 1u);
-                    if (p < LIST) {
-                        S.lkey[p] = (uint64_t)key_of(x) << 32 | (uint32_t)~j;  // greater: earlier in the order
-                        S.lw[p] = w;
-                    }
-                }
+                const int b = shift == 33 ? bins(x) : (1 << step) - 1 - (int)(key_of(x) >> low & ((1u << step) - 1));
+                if (w) atomicAdd((unsigned long long*)&S.hist[b], (unsigned long long)w);
             }
         });
         __syncthreads();
-        const int count = (int)S.listed;
+        uint64_t total;
+        const int b = find_sum<THREADS>(S, S.hist, S.BINS, r.tid, total, [&](uint64_t) { return t - above; });
+        above += S.found[0];
+        if (shift == 33) {
+            from = least_of_bin(bins, b - 1);
+            least = least_of_bin(bins, b);
+            shift = 32;
+        } else {
+            prefix = prefix << step | ((1u << step) - 1 - (uint32_t)b);
+            shift = low;
+        }
+        const int count = collect(r, S, [&](float x, int) __attribute__((always_inline)) { return member(x); }, f);
         if (count <= LIST) {
             // the last of the front is the one before which they sum to t or less and with which to more
             for (int i = r.tid; i < count; i += THREADS) {
@@ -280,38 +425,79 @@ __device__ Cut front(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint6
                 if (before <= t && before + S.lw[i] > t) S.answer = key;
             }
             __syncthreads();
-            return Cut{(uint32_t)(S.answer >> 32), (int)~(uint32_t)S.answer + 1};
+            return cut_after(S.answer);
         }
         if (shift == 0) {  // many equal values: their f are equal too, and the first of them are meant
-            uint64_t total;
-            const int last = locate(r, S, t - above, nullptr, total, [&](float x, int j) { return member(x) ? f(x, j) : 0ull; });
-            return Cut{prefix, last + 1};
+            const int last = locate(r, S, total, nullptr, t - above, [&](float x, int) __attribute__((always_inline)) { return member(x); }, f);
+            return Cut{value_of(prefix), last + 1};
         }
-        const int step = shift < BITS ? shift : BITS;
-        const int low = shift - step;
-        auto sub = [&](float x, int) __attribute__((always_inline)) {
-            return member(x) ? (1 << step) - 1 - (int)(key_of(x) >> low & ((1u << step) - 1)) : -1;
-        };
-        histogram(r, S, t - above, sub, f);
-        above += S.found[1];
-        const uint32_t digit = (1u << step) - 1 - (uint32_t)S.found[0];
-        prefix = prefix << step | digit;
-        shift = low;
     }
 }
 
+// The listed classes (the first K of the order and maybe more) reduced by top-k, top-p and min-p, and the draw. They are ranked in the
+// order, and what is kept by place. K <= count <= LIST.
 template <class T, int THREADS, bool STAGED>
-__global__ __launch_bounds__(THREADS) void sample_kernel(const T* __restrict__ logits, int C, int64_t ld, const float* __restrict__ u_rows,
+__device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, int count, int K, float P, double border,
+                           double md, float u, uint64_t& total) {
+    const int tid = r.tid;
+    constexpr int PER = Shared<THREADS>::LIST / THREADS;  // listed classes of a thread
+    for (int i = tid; i < count; i += THREADS) {
+        const uint64_t key = S.lkey[i];
+        int rank = 0;
+        for (int k = 0; k < count; ++k) rank += S.lkey[k] > key;
+        S.sorted[rank] = key;
+        S.sw[rank] = S.lw[i];
+    }
+    __syncthreads();
+    count = K;
+    // thread tid has ranks tid * PER ..
+    uint64_t own = 0;
+    for (int i = 0; i < PER; ++i)
+        if (tid * PER + i < count) own += S.sw[tid * PER + i];
+    if (P < 1.f) {
+        const uint64_t sum = group_sum<THREADS>(own, S);
+        const double q = ceil((double)P * (double)sum);
+        const uint64_t need = q >= 1.0 ? (uint64_t)q : 1;
+        uint64_t all;
+        const int last = find_sum<THREADS>(S, S.sw, count, tid, all, [&](uint64_t) { return need - 1; });
+        count = last + 1;
+        __syncthreads();
+    }
+    // by place: the kept ones before each, and their weights
+    for (int i = tid; i < count; i += THREADS) {
+        const uint64_t key = S.sorted[i];
+        const bool kept = (double)value_of((uint32_t)(key >> 32)) - md >= border;
+        S.lkey[i] = kept ? (uint32_t)~(uint32_t)key : 0xFFFFFFFFu;
+        S.lw[i] = kept ? S.sw[i] : 0;
+    }
+    __syncthreads();
+    own = 0;
+    for (int i = tid; i < count; i += THREADS) own += S.lw[i];
+    total = group_sum<THREADS>(own, S);
+    const uint64_t t = share_of(u, total);
+    for (int i = tid; i < count; i += THREADS) {
+        const uint64_t place = S.lkey[i];
+        uint64_t before = 0;
+        for (int k = 0; k < count; ++k) before += S.lkey[k] < place ? S.lw[k] : 0;
+        if (before <= t && before + S.lw[i] > t) S.answer = place;
+    }
+    __syncthreads();
+    return (int)S.answer;
+}
+
+template <class T, int THREADS, bool STAGED>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : 1) void sample_kernel(const T* __restrict__ logits, int C, int64_t ld, const float* __restrict__ u_rows,
                                                          sage_sampling how, int* __restrict__ labels, float* __restrict__ logp) {
     __shared__ Shared<THREADS> S;
-    constexpr int VL = RowType<T>::VL;
-    const int64_t row = blockIdx.x;
+    constexpr int VL = RowType<T>::VL, W = THREADS / 64, LIST = Shared<THREADS>::LIST;
     extern __shared__ u32x4 staged[];
-    const Row<T, THREADS, STAGED> r{logits + row * ld, C, (int)threadIdx.x, (C + THREADS * VL - 1) / (THREADS * VL), staged};
+    const int64_t row = blockIdx.x;
+    const Row<T, THREADS, STAGED> r{logits + row * ld, C, (int)threadIdx.x, (C + THREADS * U * VL - 1) / (THREADS * U * VL), staged};
     const float T32 = how.temperature_rows ? how.temperature_rows[row] : how.temperature;
     const float P32 = how.top_p_rows ? how.top_p_rows[row] : how.top_p;
     const float M32 = how.min_p_rows ? how.min_p_rows[row] : how.min_p;
     const int K = how.top_k_rows ? how.top_k_rows[row] : how.top_k;
+    const float u = u_rows[row];
 
     float m = -INFINITY, low = INFINITY;  // greatest, and least finite
     bool nan = false;
@@ -322,7 +508,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const T* __restrict__ l
     });
     if (nan) m = INFINITY;  // either is no distribution
     m = group_reduce<THREADS>(m, S.fpart, [](float a, float b) { return fmaxf(a, b); });
-    low = group_reduce<THREADS>(low, S.fpart + THREADS / 64, [](float a, float b) { return fminf(a, b); });
+    low = group_reduce<THREADS>(low, S.fpart + W, [](float a, float b) { return fminf(a, b); });
     if (!(fabsf(m) < INFINITY)) {
         if (r.tid == 0) {
             labels[row] = -1;
@@ -330,9 +516,10 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const T* __restrict__ l
         }
         return;
     }
-    uint64_t total;
+    uint64_t total = 0;
+    int j = -1;
     if (!(T32 > 0.f)) {
-        const int j = locate(r, S, 0, nullptr, total, [&](float x, int) { return x == m ? 1ull : 0ull; });
+        j = locate(r, S, total, nullptr, 0, [&](float x, int) __attribute__((always_inline)) { return x == m; }, [](float, int) { return 1ull; });
         if (r.tid == 0) {
             labels[row] = j;
             if (logp) logp[row] = 0.f;
@@ -341,24 +528,110 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const T* __restrict__ l
     }
     const double Td = T32, inv = 1.0 / Td, md = m;
     const float spread = fminf(m - low, 3e38f);
-    auto weight = [&](float x) __attribute__((always_inline)) { return weight_of(((double)x - md) * inv); };
-    Cut cut{0, 0};  // (no value has key 0)
-    if (K > 0 && K < C)
-        cut = front(r, S, (uint64_t)K - 1, m, fminf(spread, 64.f), [&](float, int j) __attribute__((always_inline)) { return j < C ? 1ull : 0ull; });
-    auto kept_weight = [&](float x, int j) __attribute__((always_inline)) { return cut.keeps(key_of(x), j) ? weight(x) : 0ull; };
-    if (P32 < 1.f) {
-        uint64_t s = 0;
-        r.each([&](float x, int j) __attribute__((always_inline)) { s += kept_weight(x, j); });
-        __syncthreads();
-        s = group_reduce<THREADS>(s, S.part, [](uint64_t a, uint64_t b) { return a + b; });
-        const double q = ceil((double)P32 * (double)s);
-        cut = front(r, S, q >= 1.0 ? (uint64_t)q - 1 : 0, m, fminf(spread, 30.f * T32), kept_weight);
-    }
+    auto bits = [&](float x) __attribute__((always_inline)) { return weight_bits(((double)x - md) * inv); };
+    auto weight = [&](float x, int) __attribute__((always_inline)) { return bits(x) - ROUND_BITS; };
     double border = -INFINITY;  // z - m of the least class that min-p keeps
     if (M32 > 0.f) border = Td * log((double)fminf(M32, 1.f));
-    const int j = locate(r, S, 0, u_rows + row, total, [&](float x, int k) __attribute__((always_inline)) {
-        return (double)x - md >= border ? kept_weight(x, k) : 0ull;
-    });
+    Cut cut{-INFINITY, 0};  // (-inf has no weight)
+    if (K > 0 && K < C) {
+        // the bin that the K-th is in; if all up to it can be listed, the rest is done on the list
+        const Bins bins(m, fminf(spread, 64.f), S.BINS);
+        uint32_t* counts = (uint32_t*)S.hist;
+        clear_histogram(S, r.tid);
+        r.each([&](float x, int e) __attribute__((always_inline)) {
+            if (e < C) atomicAdd(&counts[bins(x)], 1u);
+        });
+        __syncthreads();
+        uint64_t all;
+        const int b = find_sum<THREADS>(S, counts, S.BINS, r.tid, all, [&](uint64_t) { return (uint64_t)K - 1; });
+        const uint64_t through = S.found[0] + S.found[1];
+        if (through <= LIST) {
+            const float least = least_of_bin(bins, b);
+            const int count = collect(r, S, [&](float x, int e) __attribute__((always_inline)) { return (x >= least) & (e < C); },
+                                      [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) | 1ull << 63; });
+            for (int i = r.tid; i < count; i += THREADS) S.lw[i] &= ~(1ull << 63);  // (without a weight they count for top-k all the same)
+            __syncthreads();
+            j = draw_listed(r, S, count, K, P32, border, md, u, total);
+        } else {
+            cut = front(r, S, (uint64_t)K - 1, bins, [&](float, int e) __attribute__((always_inline)) { return e < C ? 1ull : 0ull; });
+        }
+    }
+    if (j < 0 && P32 < 1.f) {
+        // An approximate histogram says in which bin the border is likely to be. One exact pass then has the sum of all, for each segment the
+        // sum of what is in the bins before, and a list of the bin itself, whose kept members are added to the segments one by one.
+        const Bins bins(m, fminf(spread, 30.f * T32), S.BINS);
+        auto in_cut = [&](float x, int e) __attribute__((always_inline)) { return cut.keeps(x, e); };
+        const float c2 = (float)(inv * 1.4426950408889634);
+        clear_histogram(S, r.tid);
+        r.each([&](float x, int e) __attribute__((always_inline)) {
+            // (whole numbers: adding floats in LDS takes ten times as long)
+            const uint32_t w = (uint32_t)(__builtin_amdgcn_exp2f((x - m) * c2) * 0x1p31f);
+            if (in_cut(x, e)) atomicAdd((unsigned long long*)&S.hist[bins(x)], (unsigned long long)w);
+        });
+        __syncthreads();
+        const int b = find_sum<THREADS>(S, S.hist, S.BINS, r.tid, total, [&](uint64_t all) { return share_of(P32, all); });
+        __syncthreads();
+        if (r.tid == 0) S.listed = 0;
+        __syncthreads();
+        const float from = least_of_bin(bins, b - 1), least = least_of_bin(bins, b);
+        uint64_t sum = 0, before = 0;
+        r.visit([&](int i, const u32x4* v) __attribute__((always_inline)) {
+            uint64_t own = 0;
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+#pragma unroll
+                for (int k = 0; k < VL; ++k) {
+                    if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                    const float x = RowType<T>::at(v[q], k);
+                    const int e = r.place(i, q) + k;
+                    const uint64_t w = (bits(x) - ROUND_BITS) & mask_of(in_cut(x, e));
+                    sum += w;
+                    own += w & mask_of(x >= from);
+                    if ((x < from) & (x >= least) & (w != 0)) {
+                        const unsigned p = atomicAdd(&S.listed, 1u);
+                        if (p < LIST) {
+                            S.lkey[p] = (uint64_t)key_of(x) << 32 | (uint32_t)~e;
+                            S.lw[p] = w;
+                        }
+                    }
+                }
+            }
+            before += own;
+            const uint64_t s = wave_sum(own);
+            if ((r.tid & 63) == 0) S.seg[i * W + (r.tid >> 6)] = s;
+        });
+        sum = group_sum<THREADS>(sum, S);
+        before = group_sum<THREADS>(before, S);
+        const double q = ceil((double)P32 * (double)sum);
+        const uint64_t need = q >= 1.0 ? (uint64_t)q : 1;
+        const int listed = (int)S.listed;
+        uint64_t listed_sum = 0;
+        if (listed <= LIST) {
+            for (int i = r.tid; i < listed; i += THREADS) listed_sum += S.lw[i];
+            listed_sum = group_sum<THREADS>(listed_sum, S);
+        }
+        if (before < need && before + listed_sum >= need) {
+            for (int i = r.tid; i < listed; i += THREADS) {
+                const uint64_t key = S.lkey[i];
+                uint64_t ahead = before;
+                for (int k = 0; k < listed; ++k) ahead += S.lkey[k] > key ? S.lw[k] : 0;
+                if (ahead < need) {
+                    atomicAdd((unsigned long long*)&S.seg[r.segment_of((int)~(uint32_t)key)], (unsigned long long)S.lw[i]);
+                    if (ahead + S.lw[i] >= need) S.answer = key;
+                }
+            }
+            __syncthreads();
+            cut = cut_after(S.answer);
+            __syncthreads();
+            if ((double)cut.value - md >= border)  // (else min-p keeps less)
+                j = locate_in(r, S, total, &u, 0, [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) & mask_of(in_cut(x, e)); });
+        } else {
+            cut = front(r, S, need - 1, bins, [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) & mask_of(in_cut(x, e)); });
+        }
+    }
+    if (j < 0)
+        j = locate(r, S, total, &u, 0,
+                   [&](float x, int e) __attribute__((always_inline)) { return ((double)x - md >= border) & cut.keeps(x, e) & (e < C); }, weight);
     if (r.tid == 0) {
         labels[row] = j;
         if (logp) logp[row] = (float)(((double)RowType<T>::widen(r.z[j]) - md) * inv - log((double)total * 0x1p-42));
@@ -376,7 +649,7 @@ hipError_t launch_sample(const void* logits, int64_t rows, int C, int64_t ld, co
         const auto go = [&](auto threads, auto staged) {
             constexpr int N = decltype(threads)::value;
             constexpr bool ST = decltype(staged)::value;
-            const size_t lds = ST ? (size_t)((C + N * VL - 1) / (N * VL)) * N * 16 : 0;
+            const size_t lds = ST ? (size_t)((C + N * U * VL - 1) / (N * U * VL)) * N * U * 16 : 0;
             const auto kernel = sample_kernel<T, N, ST>;
             if (lds > 32768)
                 if (hipError_t e = ensure_dynamic_lds((const void*)kernel, 65536); e != hipSuccess) return e;
@@ -388,7 +661,7 @@ hipError_t launch_sample(const void* logits, int64_t rows, int C, int64_t ld, co
         if (C <= 64 * 4 * VL) e = go(integral_constant<int, 64>{}, std::true_type{});
         else if (C <= 256 * 4 * VL) e = go(integral_constant<int, 256>{}, std::true_type{});
         else if (C <= 1024 * 4 * VL) e = go(integral_constant<int, 1024>{}, std::true_type{});
-        else e = go(integral_constant<int, 1024>{}, std::false_type{});
+        else e = go(integral_constant<int, 512>{}, std::false_type{});
         if (e != hipSuccess) return e;
         if (h.temperature_rows) h.temperature_rows += grid.x;
         if (h.top_k_rows) h.top_k_rows += grid.x;
