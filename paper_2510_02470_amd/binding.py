@@ -415,27 +415,37 @@ def _need(ok, what):
 
 
 def _code(torch, dtype, what):
-    _need(dtype in (torch.float32, torch.bfloat16), what)
-    return SAGE_BF16 if dtype == torch.bfloat16 else SAGE_F32
+    if dtype is torch.float32:
+        return SAGE_F32
+    _need(dtype is torch.bfloat16, what)
+    return SAGE_BF16
 
 
-def _here(torch, t, what, dtype=None, shape=None):
-    """t is a tensor on the current device (of a type and shape, contiguous, if they are given)."""
-    _need(torch.is_tensor(t) and t.is_cuda and t.device.index == torch.cuda.current_device(), what)
-    _need(dtype is None or t.dtype == dtype, what)
-    _need(shape is None or (tuple(t.shape) == tuple(shape) and t.is_contiguous()), what)
-    return t
+def _device(torch, t, what):
+    """The current device, which t has to be on."""
+    _need(isinstance(t, torch.Tensor) and t.is_cuda, what)
+    dev = torch._C._cuda_getDevice()
+    _need(t.get_device() == dev, what)
+    return dev
 
 
-def _logits(torch, logits, what):
+def _rows_address(torch, t, dev, dtype, rows, what):
+    """Address of a tensor of one value per row."""
+    if not (isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype is dtype and t.shape == (rows,) and t.is_contiguous()):
+        _need(False, what)
+    return t.data_ptr()
+
+
+def _logits(torch, t, dev, what):
     """rows x classes with classes next to each other -> (type code, rows, classes, stride of the rows)"""
-    _here(torch, logits, what)
-    _need(logits.dim() == 2 and logits.shape[1] >= 1, what)
-    rows, classes = logits.shape
-    _need(classes == 1 or logits.stride(1) == 1, what)
-    ld = logits.stride(0) if rows > 1 else classes
-    _need(ld >= classes, what)
-    return _code(torch, logits.dtype, what), rows, classes, ld
+    if not (isinstance(t, torch.Tensor) and t.get_device() == dev and t.dim() == 2):
+        _need(False, what)
+    rows, classes = t.shape
+    sr, sc = t.stride()
+    ld = sr if rows > 1 else classes
+    if not (classes >= 1 and (sc == 1 or classes == 1) and ld >= classes):
+        _need(False, what)
+    return _code(torch, t.dtype, what), rows, classes, ld
 
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
@@ -448,20 +458,33 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     import torch
 
     what = "sage_sample"
-    code, rows, classes, ld = _logits(torch, logits, what)
-    _here(torch, u, what, torch.float32, (rows,))
+    dev = _device(torch, logits, what)
+    code, rows, classes, ld = _logits(torch, logits, dev, what)
+    f32 = torch.float32
+    u_address = _rows_address(torch, u, dev, f32, rows, what)
     how = SageSampling()
-    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                               ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
-        if torch.is_tensor(value):
-            setattr(how, name + "_rows", _here(torch, value, what, dtype, (rows,)).data_ptr())
-        elif name == "top_k":
-            how.top_k = max(0, min(int(value), 0x7FFFFFFF))
-        else:
-            setattr(how, name, float(value))
-    labels = torch.empty(rows, dtype=torch.int32, device=logits.device)
-    logp = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    _check(lib().sage_sample(_ptr(logits), code, rows, classes, ld, _ptr(u), C.byref(how), _ptr(labels), _ptr(logp), _stream(torch)), what)
+    if isinstance(temperature, torch.Tensor):
+        how.temperature_rows = _rows_address(torch, temperature, dev, f32, rows, what)
+    else:
+        how.temperature = temperature
+    if isinstance(top_k, torch.Tensor):
+        how.top_k_rows = _rows_address(torch, top_k, dev, torch.int32, rows, what)
+    else:
+        how.top_k = max(0, min(int(top_k), 0x7FFFFFFF))
+    if isinstance(top_p, torch.Tensor):
+        how.top_p_rows = _rows_address(torch, top_p, dev, f32, rows, what)
+    else:
+        how.top_p = top_p
+    if isinstance(min_p, torch.Tensor):
+        how.min_p_rows = _rows_address(torch, min_p, dev, f32, rows, what)
+    else:
+        how.min_p = min_p
+    labels = torch.empty(rows, dtype=torch.int32, device="cuda")
+    logp = torch.empty(rows, dtype=f32, device="cuda")
+    rc = lib().sage_sample(logits.data_ptr(), code, rows, classes, ld, u_address, C.byref(how), labels.data_ptr(), logp.data_ptr(),
+                           torch._C._cuda_getCurrentRawStream(dev))
+    if rc != SAGE_OK:
+        _check(rc, what)
     return labels, logp
 
 
@@ -475,27 +498,30 @@ def logit_error(logits, labels, weights=None, out=None, dtype=None):
     import torch
 
     what = "sage_logit_error"
-    code, rows, classes, ld = _logits(torch, logits, what)
-    _here(torch, labels, what, torch.int32, (rows,))
-    if weights is not None:
-        _here(torch, weights, what, torch.float32, (rows,))
+    dev = _device(torch, logits, what)
+    code, rows, classes, ld = _logits(torch, logits, dev, what)
+    labels_address = _rows_address(torch, labels, dev, torch.int32, rows, what)
+    weights_address = None if weights is None else _rows_address(torch, weights, dev, torch.float32, rows, what)
     if out is None:
-        out = torch.empty((rows, classes), dtype=logits.dtype if dtype is None else dtype, device=logits.device)
-    e_code, e_rows, e_classes, e_ld = _logits(torch, out, what)
-    _need((e_rows, e_classes) == (rows, classes) and (dtype is None or out.dtype == dtype), what)
-    loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    _check(lib().sage_logit_error(_ptr(logits), code, rows, classes, ld, _ptr(labels), _ptr(weights), _ptr(out), e_code, e_ld, _ptr(loss),
-                                  _stream(torch)), what)
+        out = torch.empty((rows, classes), dtype=logits.dtype if dtype is None else dtype, device="cuda")
+        e_code, e_ld = code if dtype is None else _code(torch, dtype, what), classes
+    else:
+        e_code, e_rows, e_classes, e_ld = _logits(torch, out, dev, what)
+        _need(e_rows == rows and e_classes == classes and (dtype is None or out.dtype is dtype), what)
+    loss = torch.empty(rows, dtype=torch.float32, device="cuda")
+    rc = lib().sage_logit_error(logits.data_ptr(), code, rows, classes, ld, labels_address, weights_address, out.data_ptr(), e_code, e_ld,
+                                loss.data_ptr(), torch._C._cuda_getCurrentRawStream(dev))
+    if rc != SAGE_OK:
+        _check(rc, what)
     return out, loss
 
 
 MUON = (3.4445, -4.7750, 2.0315)  # of a step of orthogonalize: singular values end between about 0.7 and 1.2
 
 
-def _matrices(torch, G, what):
+def _matrices(torch, G, dev, what):
     """A matrix, or several, with rows or columns next to each other -> (batch, rows, cols, ld, stride, transposed)"""
-    _here(torch, G, what)
-    _need(G.dim() in (2, 3) and G.shape[-2] >= 1 and G.shape[-1] >= 1, what)
+    _need(isinstance(G, torch.Tensor) and G.get_device() == dev and G.dim() in (2, 3) and G.shape[-2] >= 1 and G.shape[-1] >= 1, what)
     rows, cols = G.shape[-2:]
     batch = G.shape[0] if G.dim() == 3 else 1
     sr, sc = G.stride(-2), G.stride(-1)
@@ -526,20 +552,21 @@ def orthogonalize(G, steps=5, coefficients=MUON, eps=1e-7, scale=1.0, out=None):
         triples = [triples] * max(steps, 0)
     _need(len(triples) == steps and all(len(t) == 3 for t in triples), what)
     flat = [float(v) for t in triples for v in t]
-    batch, rows, cols, ld, stride, turned = _matrices(torch, G, what)
+    dev = _device(torch, G, what)
+    batch, rows, cols, ld, stride, turned = _matrices(torch, G, dev, what)
     code = _code(torch, G.dtype, what)
     if out is None:
-        out = torch.empty(G.shape[:-2] + (rows, cols), dtype=G.dtype, device=G.device)
+        out = torch.empty(G.shape[:-2] + (rows, cols), dtype=G.dtype, device="cuda")
         out = out.transpose(-1, -2) if turned else out
-    _need(out.dtype == G.dtype and out.shape == G.shape, what)
-    o_batch, o_rows, o_cols, o_ld, o_stride, o_turned = _matrices(torch, out, what)
+    _need(isinstance(out, torch.Tensor) and out.dtype is G.dtype and out.shape == G.shape, what)
+    o_batch, o_rows, o_cols, o_ld, o_stride, o_turned = _matrices(torch, out, dev, what)
     if o_turned != turned and 1 in (rows, cols):  # a single row or column may be called either
         o_rows, o_cols, o_ld, o_turned = o_cols, o_rows, max(o_ld, o_cols), turned
     _need(o_turned == turned, what)
     L = lib()
     need = C.c_size_t(0)
     _check(L.sage_orthogonalize_work(code, batch, rows, cols, C.byref(need)), what)
-    work = torch.empty(max(need.value, 1), dtype=torch.uint8, device=G.device)
-    _check(L.sage_orthogonalize(_ptr(G), code, batch, rows, cols, ld, stride, (C.c_float * len(flat))(*flat), steps, float(eps), float(scale),
-                                _ptr(out), o_ld, o_stride, C.c_void_p(work.data_ptr()), need.value, _stream(torch)), what)
+    work = torch.empty(max(need.value, 1), dtype=torch.uint8, device="cuda")
+    _check(L.sage_orthogonalize(G.data_ptr(), code, batch, rows, cols, ld, stride, (C.c_float * len(flat))(*flat), steps, eps, scale,
+                                out.data_ptr(), o_ld, o_stride, work.data_ptr(), need.value, torch._C._cuda_getCurrentRawStream(dev)), what)
     return out

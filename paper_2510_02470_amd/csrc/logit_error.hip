@@ -4,7 +4,11 @@
 //     loss = ln((R + e_y) / e_y) = log1p(R / e_y),   E_j = w e_j / (R + e_y),   E_y = -w R / (R + e_y).
 // The label is left out of the sum, because loss and E_y are differences of nearly equal numbers when written with p_y: a
 // learnt example has p_y = 1 - 1e-6, of which fp32 keeps one digit of the part that matters.
+//
+// Bound by memory: a row is read once and its gradient written once. A work-group keeps its row in registers between the two,
+// as it was read, and forms the exponentials twice.
 #include <algorithm>
+#include <type_traits>
 
 #include "logit_rows.h"
 #include "sage_internal.h"
@@ -12,15 +16,16 @@
 namespace sage {
 namespace {
 
-constexpr int EB = 1024;
-
-// e^(x - m): the difference is exact or rounded once; the product with log2 e is carried to twice the width.
+// e^(x - m): the difference is exact or rounded once; the product with log2 e is carried to twice the width where WIDE (a bf16 result
+// does not show the 2^-20 that a difference of 16 loses otherwise).
+template <bool WIDE>
 __device__ __forceinline__ float exp_diff(float x, float m) {
     const float d = x - m;
     const float L = 1.44269502f, L2 = 1.92596299e-8f;  // log2 e = L + L2
     const float t = d * L;
-    const float r = fmaf(d, L, -t) + d * L2;
     const float e = __builtin_amdgcn_exp2f(t);
+    if constexpr (!WIDE) return e;
+    const float r = fmaf(d, L, -t) + d * L2;
     return t <= -126.f ? 0.f : fmaf(e, r * 0.693147181f, e);  // (r is no number where d is infinite; a NaN stays one)
 }
 
@@ -31,70 +36,184 @@ __device__ __forceinline__ float row_loss(float rest, float ey, float zy, float 
     return (float)log1p((double)rest / (double)ey);
 }
 
-// One work-group a row: maximum, sum, and the row again for the answer.
-template <class T, class TE>
-__global__ __launch_bounds__(EB) void logit_error_kernel(const T* logits, int64_t C, int64_t ld, const int* __restrict__ labels,
-                                                         const float* __restrict__ weights, TE* E, int64_t ldE, float* __restrict__ loss) {
-    __shared__ float part[2][EB / 64];
-    const int64_t row = blockIdx.x;
-    const T* z = logits + row * ld;
-    TE* out = E ? E + row * ldE : nullptr;
-    const int y = labels[row];
-    const int tid = threadIdx.x;
-    if (y < 0) {
-        if (out)
-            for (int64_t j = tid; j < C; j += EB) out[j] = 0;
-        if (loss && tid == 0) loss[row] = 0.f;
-        return;
-    }
+template <class T>
+struct ErrorArgs {
+    const T* logits;
+    int C;
+    int64_t ld;
+    const int* labels;
+    const float* weights;
+    int64_t ldE;
+    float* loss;
+};
+
+// A row's vector from e0 on; what lies behind the end is -inf. whole: it is known not to reach there.
+template <class T>
+__device__ __forceinline__ u32x4 row_vector(const T* z, int e0, int n, bool whole) {
     constexpr int VL = RowType<T>::VL;
-    const bool known = y < C;
-    const float zy = known ? RowType<T>::widen(z[y]) : __builtin_nanf("");
-    float m = zy;
-    for (int64_t e0 = (int64_t)tid * VL; e0 < C; e0 += EB * VL) {
-        float x[VL];
-        row_floats(z, e0, C, -INFINITY, x);
+    if (whole || e0 + VL <= n) return load16(z + e0);
+    constexpr uint32_t NONE = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+    u32x4 v = {NONE, NONE, NONE, NONE};
 #pragma unroll
-        for (int i = 0; i < VL; ++i) m = fmaxf(m, x[i]);
-    }
-    m = group_reduce<EB>(m, part[0], [](float a, float b) { return fmaxf(a, b); });
-    if (m == -INFINITY) m = 0.f;  // no class is possible: every e is 0
-    float rest = 0.f;
-    for (int64_t e0 = (int64_t)tid * VL; e0 < C; e0 += EB * VL) {
-        float x[VL];
-        row_floats(z, e0, C, -INFINITY, x);
+    for (int i = 0; i < VL; ++i)
+        if (e0 + i < n) {
+            if constexpr (sizeof(T) == 2) v[i >> 1] = i & 1 ? (v[i >> 1] & 0xFFFFu) | (uint32_t)z[e0 + i] << 16 : (v[i >> 1] & 0xFFFF0000u) | z[e0 + i];
+            else v[i] = __float_as_uint(z[e0 + i]);
+        }
+    return v;
+}
+
+// -inf in the label's place, if it is in this vector.
+template <class T>
+__device__ __forceinline__ void drop_label(u32x4& v, int at) {
+    constexpr int VL = RowType<T>::VL;
+    if ((unsigned)at >= (unsigned)VL) return;
 #pragma unroll
-        for (int i = 0; i < VL; ++i) rest += e0 + i == y ? 0.f : exp_diff(x[i], m);
-    }
-    rest = group_reduce<EB>(rest, part[1], [](float a, float b) { return a + b; });
-    const float ey = exp_diff(zy, m), S = rest + ey;
-    if (loss && tid == 0) loss[row] = row_loss(rest, ey, zy, m);
-    if (!out) return;
-    const float f = weights ? weights[row] : 1.f;
-    const float scale = S == 0.f ? 0.f : f / S;
-    for (int64_t e0 = (int64_t)tid * VL; e0 < C; e0 += EB * VL) {
-        float x[VL];
-        row_floats(z, e0, C, -INFINITY, x);
-#pragma unroll
-        for (int i = 0; i < VL; ++i)
-            if (e0 + i < C) out[e0 + i] = RowType<TE>::narrow(e0 + i == y ? -scale * rest : scale * exp_diff(x[i], m));
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) {
+            if (at == 2 * i) v[i] = (v[i] & 0xFFFF0000u) | 0xFF80u;
+            if (at == 2 * i + 1) v[i] = (v[i] & 0xFFFFu) | 0xFF800000u;
+        } else {
+            if (at == i) v[i] = 0xFF800000u;
+        }
     }
 }
 
-}  // namespace
+template <class T, class TE>
+__device__ __forceinline__ void write_vector(TE* out, int e0, int n, bool whole, const u32x4& v, float scale, float m) {
+    constexpr int VL = RowType<T>::VL;
+    constexpr bool WIDE = sizeof(TE) == 4;
+    TE h[VL];
+#pragma unroll
+    for (int i = 0; i < VL; ++i) h[i] = RowType<TE>::narrow(scale * exp_diff<WIDE>(RowType<T>::at(v, i), m));
+    if (whole || e0 + VL <= n) {
+        __builtin_memcpy(out + e0, h, sizeof(h));
+    } else {
+#pragma unroll
+        for (int i = 0; i < VL; ++i)
+            if (e0 + i < n) out[e0 + i] = h[i];
+    }
+}
+
+// One work-group a row. N > 0: N vectors of 16 bytes a thread, kept in registers between reading and writing; 0: a longer row, read a
+// second and a third time.
+template <class T, class TE, int THREADS, int N>
+__global__ __launch_bounds__(THREADS) void logit_error_kernel(ErrorArgs<T> a, TE* E) {
+    __shared__ float2 part[THREADS / 64];
+    constexpr int VL = RowType<T>::VL;
+    constexpr bool WIDE = sizeof(TE) == 4;
+    const int64_t row = blockIdx.x;
+    const T* z = a.logits + row * a.ld;
+    TE* out = E ? E + row * a.ldE : nullptr;
+    const int y = a.labels[row], C = a.C;
+    const int tid = threadIdx.x;
+    if (y < 0) {
+        if (out)
+            for (int j = tid; j < C; j += THREADS) out[j] = 0;
+        if (a.loss && tid == 0) a.loss[row] = 0.f;
+        return;
+    }
+    const float zy = y < C ? RowType<T>::widen(z[y]) : __builtin_nanf("");
+    const float f = a.weights ? a.weights[row] : 1.f;
+    const int turns = (C + THREADS * VL - 1) / (THREADS * VL);
+    u32x4 reg[N > 0 ? N : 1];
+    // the greatest logit so far and the sum of the exponentials relative to it, together as the vectors arrive; m is finite from the
+    // start, so that a difference to it is a number where all logits are -inf
+    float m = fmaxf(zy, -3.40282347e38f), rest = 0.f;
+    // f(vector, its first element, whether all vectors of the wave are whole); FIRST: the pass that reads, and puts -inf in the label's place
+    const int first = __builtin_amdgcn_readfirstlane(tid) * VL;  // of the wave
+    auto visit = [&](auto first_pass, auto f) __attribute__((always_inline)) {
+        constexpr bool FIRST = decltype(first_pass)::value;
+        if constexpr (N > 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int w0 = i * THREADS * VL + first, e0 = (i * THREADS + tid) * VL;
+                // (turns mixed with each other, or floats kept from one pass to the next, would need more registers)
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("" : "+v"(reg[i]));
+                if (FIRST && (unsigned)(y - w0) < 64u * VL) drop_label<T>(reg[i], y - e0);
+                f(reg[i], e0, w0 + 64 * VL <= C);
+            }
+        } else {
+            for (int i = 0; i < turns; ++i) {
+                const int w0 = i * THREADS * VL + first, e0 = (i * THREADS + tid) * VL;
+                u32x4 v = row_vector(z, e0, C, w0 + 64 * VL <= C);
+                if (FIRST && (unsigned)(y - w0) < 64u * VL) drop_label<T>(v, y - e0);
+                f(v, e0, w0 + 64 * VL <= C);
+            }
+        }
+    };
+    if constexpr (N > 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) reg[i] = row_vector(z, (i * THREADS + tid) * VL, C, i * THREADS * VL + first + 64 * VL <= C);
+    }
+    visit(std::true_type{}, [&](const u32x4& v, int, bool) __attribute__((always_inline)) {
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < VL; ++i) top = fmaxf(top, RowType<T>::at(v, i));
+        float sum = rest * exp_diff<WIDE>(m, top);
+#pragma unroll
+        for (int i = 0; i < VL; ++i) sum += exp_diff<WIDE>(RowType<T>::at(v, i), top);
+        m = top;
+        rest = sum;
+    });
+    // over the wave, then over the work-group
+    float top = m;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    rest *= exp_diff<WIDE>(m, top);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) rest += __shfl_xor(rest, d, 64);
+    m = top;
+    if constexpr (THREADS > 64) {
+        if ((tid & 63) == 0) part[tid >> 6] = float2{m, rest};
+        __syncthreads();
+        float2 w[THREADS / 64];
+#pragma unroll
+        for (int i = 0; i < THREADS / 64; ++i) w[i] = part[i];
+#pragma unroll
+        for (int i = 0; i < THREADS / 64; ++i) m = fmaxf(m, w[i].x);
+        rest = 0.f;
+#pragma unroll
+        for (int i = 0; i < THREADS / 64; ++i) rest += w[i].y * exp_diff<WIDE>(w[i].x, m);
+    }
+    const float ey = exp_diff<true>(zy, m), S = rest + ey;
+    if (a.loss && tid == 0) a.loss[row] = row_loss(rest, ey, zy, m);
+    if (!out) return;
+    const float scale = S == 0.f ? 0.f : f / S;
+    visit(std::false_type{}, [&](const u32x4& v, int e0, bool whole) __attribute__((always_inline)) {
+        write_vector<T>(out, e0, C, whole, v, scale, m);
+    });
+    // the label's entry, by the thread that has written its vector: after that one's store
+    if (y < C && tid == y / VL % THREADS) out[y] = RowType<TE>::narrow(-scale * rest);
+}
 
 template <class T, class TE>
-static hipError_t launch(const void* z, int64_t rows, int64_t C, int64_t ld, const int* labels, const float* weights, void* E,
-                         int64_t ldE, float* loss, hipStream_t st) {
+hipError_t launch(const void* z, int64_t rows, int64_t C, int64_t ld, const int* labels, const float* weights, void* E, int64_t ldE,
+                  float* loss, hipStream_t st) {
+    constexpr int VL = RowType<T>::VL;
     for (int64_t r0 = 0; r0 < rows; r0 += LOGIT_LAUNCH_ROWS) {
         const dim3 grid((unsigned)std::min(rows - r0, LOGIT_LAUNCH_ROWS));
-        logit_error_kernel<T, TE><<<grid, EB, 0, st>>>((const T*)z + r0 * ld, C, ld, labels + r0, weights ? weights + r0 : nullptr,
-                                                       E ? (TE*)E + r0 * ldE : nullptr, ldE, loss ? loss + r0 : nullptr);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        const ErrorArgs<T> a{(const T*)z + r0 * ld, (int)C, ld, labels + r0, weights ? weights + r0 : nullptr, ldE, loss ? loss + r0 : nullptr};
+        TE* e = E ? (TE*)E + r0 * ldE : nullptr;
+        const auto go = [&](auto threads, auto n) {
+            logit_error_kernel<T, TE, decltype(threads)::value, decltype(n)::value><<<grid, decltype(threads)::value, 0, st>>>(a, e);
+        };
+        using std::integral_constant;
+        const int64_t vectors = (C + VL - 1) / VL;
+        if (vectors <= 64) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+        else if (vectors <= 256) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+        else if (vectors <= 1024) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+        else if (vectors <= 4096) go(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+        else if (vectors <= 8192) go(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+        else if (vectors <= 16384) go(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+        else go(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
+        if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
     }
     return hipSuccess;
 }
 
+}  // namespace
 }  // namespace sage
 
 extern "C" int sage_logit_error(const void* logits, sage_dtype dtype, int64_t rows, int64_t n_classes, int64_t ld, const int32_t* labels,

@@ -22,12 +22,7 @@ struct RowType<uint16_t> {
     static constexpr int VL = 8;
     __device__ static float at(const u32x4& v, int i) { return __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16); }
     __device__ static float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-    // to nearest, ties to even; a NaN stays one
-    __device__ static uint16_t narrow(float x) {
-        const uint32_t u = __float_as_uint(x);
-        if (x != x) return (uint16_t)(u >> 16 | 0x40);
-        return (uint16_t)((u + 0x7FFF + (u >> 16 & 1)) >> 16);
-    }
+    __device__ static uint16_t narrow(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }  // to nearest, ties to even
 };
 
 // 16 bytes at an address that is aligned to an element only (one load or store: gfx9 takes any alignment in global memory)
