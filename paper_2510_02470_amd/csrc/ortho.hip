@@ -11,7 +11,7 @@
 // of 2^-40 U. (bf16 parts would need three of them, six products.)
 //
 // Layout: 32 columns of a row are 128 bytes, their 32 hi parts and then their 32 lo parts; rows and columns are padded with zeros to
-// multiples of 128. X is kept row by row for A and column by column for P X: the instructions take both factors along the
+// multiples of the tiles' side. X is kept row by row for A and column by column for P X: the instructions take both factors along the
 // summed index.
 #include <math.h>
 
@@ -25,10 +25,10 @@ namespace {
 typedef _Float16 f16;
 typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int PAD = 128;
 constexpr int KB = 32;  // columns of a block of 128 bytes
 
 // A padded matrix in parts: element (r, k) is p[r * pitch + (k / 32) * 64 + k % 32] + the one 32 further.
@@ -93,8 +93,12 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(const T* __restrict__ 
     const int64_t b = blockIdx.x / (tiles_r * tiles_c);
     const int at = blockIdx.x % (tiles_r * tiles_c);
     const int64_t r0 = (int64_t)(at / tiles_c) * 64, c0 = (int64_t)(at % tiles_c) * 64;
-    double s = 0.0;
-    for (int i = 0; i < groups; ++i) s += partial[b * groups + i];
+    __shared__ double part[4];
+    double s = (int)threadIdx.x < groups ? partial[b * groups + threadIdx.x] : 0.0;
+    for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = part[0] + part[1] + part[2] + part[3];
     const double inv = s > 0.0 || s != s ? scale / (sqrt(s) + eps) : 0.0;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const T* g = G + b * stride;
@@ -142,17 +146,23 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
     j = t - (int)((int64_t)i * (i + 1) / 2);
 }
 
+constexpr int wait_for_loads(int left) { return (left & 15) | (left >> 4) << 14 | 0x0F70; }  // until so many are on their way
+
 // C = A B^T of padded matrices in parts, both along the summed index: tiles of 32 WR RB x 32 WC CB, WR x WC waves with RB x CB
-// instruction tiles of 32 x 32 each. Blocks of 32 of the summed index go straight to LDS, one on its way while one is multiplied; a row's
+// instruction tiles of 32 x 32 each. Blocks of 32 of the summed index go straight to LDS, NST - 1 on their way while one is multiplied; a row's
 // eight pieces of 16 bytes are stored in an order turned by the row's number, so that the reads of eight rows meet
-// different banks. (The loads deposit in lane order: it is their addresses that are turned.)
-template <int WR, int WC, int RB, int CB, int MODE>
-__global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin) {
+// different banks. (The loads deposit in lane order: it is their addresses that are turned.) KS > 1: as many such groups of waves take the
+// blocks of the summed index in turn, and the first adds up what they have: a tile alone on a CU waits for its own loads and LDS
+// reads most of the time.
+template <int WR, int WC, int RB, int CB, int KS, int NST, int MODE>
+__global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin) {
     constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, THREADS = WR * WC * 64;
     constexpr int STAGE = (TM + TN) * 8;  // pieces of 16 bytes
     constexpr int LOADS = STAGE / THREADS;
     static_assert(STAGE % THREADS == 0 && TM * 8 % THREADS == 0, "whole loads");
-    extern __shared__ u32x4 lds[];  // 2 * STAGE
+    static_assert(LOADS * (NST - 2) < 64, "a wait counts up to 63");
+    static_assert(KS == 1 || (KS - 1) * RB * CB * 4 * THREADS <= KS * NST * STAGE, "room for the sums");
+    extern __shared__ u32x4 lds[];  // KS * NST * STAGE
     constexpr bool SYM = MODE == GRAM || MODE == POLY;
     const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
     const int64_t b = blockIdx.x / per;
@@ -164,10 +174,12 @@ __global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Pa
         ti = at / tiles_c;
         tj = at % tiles_c;
     }
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int group = KS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
+    const int tid = threadIdx.x - group * THREADS, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, h = lane >> 5;
     const int wr = wave / WC, wc = wave % WC;
+    u32x4* const ring = lds + group * NST * STAGE;
 
     const f16* src[LOADS];
 #pragma unroll
@@ -180,7 +192,7 @@ __global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Pa
 #pragma unroll
         for (int q = 0; q < LOADS; ++q)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[q] + (int64_t)kb * 64),
-                                             (__attribute__((address_space(3))) void*)(lds + buf * STAGE + q * THREADS + wave * 64), 16, 0, 0);
+                                             (__attribute__((address_space(3))) void*)(ring + buf * STAGE + q * THREADS + wave * 64), 16, 0, 0);
     };
 
     f32x16 acc[RB][CB];
@@ -191,17 +203,22 @@ __global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Pa
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    stage(0, 0);
+    // (beyond the end the last block is loaded again and not used, so that every turn waits for the same number of loads)
+#pragma unroll
+    for (int i = 0; i < NST - 1; ++i) stage(min(i * KS + group, kblocks - 1), i);
     const int arow = wr * 32 * RB + l32, brow = TM + wc * 32 * CB + l32;
-    for (int kb = 0; kb < kblocks; ++kb) {
+    int buf = 0;
+    for (int kb = group; kb < kblocks + group; kb += KS) {
         // this block has landed; everyone is done with the buffer of the one before
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0F70);
+        __builtin_amdgcn_s_waitcnt(wait_for_loads(LOADS * (NST - 2)));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if (kb + 1 < kblocks) stage(kb + 1, (kb + 1) & 1);
-        const u32x4* st = lds + (kb & 1) * STAGE;
+        stage(min(kb + (NST - 1) * KS, kblocks - 1), buf == 0 ? NST - 1 : buf - 1);
+        const u32x4* st = ring + buf * STAGE;
+        buf = buf == NST - 1 ? 0 : buf + 1;
+        if (KS > 1 && kb >= kblocks) continue;  // (the last turn has blocks for some groups only)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             f16x8 a[RB][2], c[CB][2];
@@ -226,6 +243,36 @@ __global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Pa
 #pragma unroll
                 for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], c[j][0], acc[i][j], 0, 0, 0);
         }
+    }
+
+    __builtin_amdgcn_s_waitcnt(wait_for_loads(0));  // nothing on its way to LDS when the work-group ends or uses it otherwise
+    if constexpr (KS > 1) {
+        f32x4* sums = (f32x4*)lds;
+        __syncthreads();
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < CB; ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        sums[(((group - 1) * RB + i) * CB + j) * 4 * THREADS + g * THREADS + tid] =
+                            f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int q = 0; q < KS - 1; ++q)
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < CB; ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 v = sums[((q * RB + i) * CB + j) * 4 * THREADS + g * THREADS + tid];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] += v[e];
+                    }
     }
 
     // A lane has four consecutive rows of one column: entries 4 g .. 4 g + 3 are rows 8 g + 4 h + 0 .. 3.
@@ -290,23 +337,35 @@ __global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Pa
 constexpr int MAX_SIDE = 32768, MAX_STEPS = 32;
 constexpr int64_t WORK_LIMIT = 1ll << 30;  // batches are taken in chunks that need no more, or one matrix at a time
 
+template <int MODE>
+int64_t tiles_of(int64_t rows, int64_t cols, int64_t side) {
+    const int64_t r = rows / side;
+    return MODE == GRAM || MODE == POLY ? r * (r + 1) / 2 : r * (cols / side);
+}
+
 struct Plan {
     int64_t m, n, M, N;  // the sides, smaller first, and padded
+    bool big;            // tiles of 128 x 128, else 64 x 64
     int groups;          // of rows, for the norm
     int64_t x, a;        // halves of X (either way) and of A
     int64_t per;         // bytes of one matrix
     int64_t chunk;       // matrices at a time
 };
 
-int64_t padded(int64_t v) { return (v + PAD - 1) / PAD * PAD; }
+int64_t padded(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
+
+// tiles of 128 x 128 of X, from which on they are used
+constexpr int64_t BIG_FROM = 256;
 
 Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     Plan p;
     p.m = std::min(rows, cols);
     p.n = std::max(rows, cols);
-    p.M = padded(p.m);
-    p.N = padded(p.n);
+    const int64_t tiles = (p.m + 127) / 128 * ((p.n + 127) / 128) * batch;
+    p.big = tiles >= BIG_FROM;
+    p.M = padded(p.m, p.big ? 128 : 64);
+    p.N = padded(p.n, p.big ? 128 : 64);
     p.groups = (int)std::min<int64_t>(rows, std::max<int64_t>(1, std::min<int64_t>(256, rows * cols / 4096)));
     p.x = 2 * p.M * p.N;
     p.a = 2 * p.M * p.M;
@@ -344,16 +403,23 @@ double scale_for(double top) {
     return ldexp(1.0, 15 - e);
 }
 
-template <int MODE>
-hipError_t product(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, hipStream_t st) {
-    constexpr int WR = 2, WC = 2, RB = 2, CB = 2;
-    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, BYTES = 2 * (TM + TN) * 128;
-    const auto kernel = ortho_product_kernel<WR, WC, RB, CB, MODE>;
+template <int MODE, int RB, int KS, int NST>
+hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, hipStream_t st) {
+    constexpr int WR = 2, WC = 2, CB = RB;
+    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, BYTES = KS * NST * (TM + TN) * 128;
+    const auto kernel = ortho_product_kernel<WR, WC, RB, CB, KS, NST, MODE>;
     if (hipError_t e = ensure_dynamic_lds((const void*)kernel, BYTES); e != hipSuccess) return e;
     const int tr = (int)(rows / TM), tc = (int)(cols / TN);
-    const int64_t per = MODE == GRAM || MODE == POLY ? (int64_t)tr * (tr + 1) / 2 : (int64_t)tr * tc;
-    kernel<<<dim3((unsigned)(per * batch)), WR * WC * 64, BYTES, st>>>(A, B, (int)(k / KB), tr, tc, fin);
+    kernel<<<dim3((unsigned)(tiles_of<MODE>(rows, cols, TM) * batch)), KS * WR * WC * 64, BYTES, st>>>(A, B, (int)(k / KB), tr, tc, fin);
     return hipGetLastError();
+}
+
+template <int MODE>
+hipError_t product(const Plan& p, const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin,
+                   hipStream_t st) {
+    if (p.big && tiles_of<MODE>(rows, cols, 128) * batch >= BIG_FROM) return product_of<MODE, 2, 1, 2>(A, B, rows, cols, k, batch, fin, st);
+    if (tiles_of<MODE>(rows, cols, 64) * batch <= 256 && k >= 8 * KB) return product_of<MODE, 1, 4, 2>(A, B, rows, cols, k, batch, fin, st);
+    return product_of<MODE, 1, 1, 3>(A, B, rows, cols, k, batch, fin, st);
 }
 
 template <class T>
@@ -383,25 +449,25 @@ hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t c
         if (cc != 0.0) {
             f.f = (float)(sa / (sx * sx));
             f.C = A;
-            if (hipError_t e = product<GRAM>(X, X, p.M, p.M, p.N, batch, f, st); e != hipSuccess) return e;
+            if (hipError_t e = product<GRAM>(p, X, X, p.M, p.M, p.N, batch, f, st); e != hipSuccess) return e;
             f.f = (float)(cc * sp / (sa * sa));
             f.fa = (float)(cb * sp / sa);
             f.diag = (float)(ca * sp);
             f.A = A;
             f.C = P;
-            if (hipError_t e = product<POLY>(A, A, p.M, p.M, p.M, batch, f, st); e != hipSuccess) return e;
+            if (hipError_t e = product<POLY>(p, A, A, p.M, p.M, p.M, batch, f, st); e != hipSuccess) return e;
         } else {
             f.f = (float)(cb * sp / (sx * sx));
             f.diag = (float)(ca * sp);
             f.C = P;
-            if (hipError_t e = product<GRAM>(X, X, p.M, p.M, p.N, batch, f, st); e != hipSuccess) return e;
+            if (hipError_t e = product<GRAM>(p, X, X, p.M, p.M, p.N, batch, f, st); e != hipSuccess) return e;
         }
         const Parts& xt = Xt[s & 1];
         if (s + 1 < steps) {
             f.f = (float)(sn / (sp * sx));
             f.C = X;
             f.Ct = Xt[(s + 1) & 1];
-            if (hipError_t e = product<STEP>(P, xt, p.M, p.N, p.M, batch, f, st); e != hipSuccess) return e;
+            if (hipError_t e = product<STEP>(p, P, xt, p.M, p.N, p.M, batch, f, st); e != hipSuccess) return e;
         } else {
             f.f = (float)(scale / (sp * sx));
             f.out = out;
@@ -410,7 +476,7 @@ hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t c
             f.rows = rows;
             f.cols = cols;
             f.out16 = sizeof(T) == 2;
-            const hipError_t e = tall ? product<LAST>(xt, P, p.N, p.M, p.M, batch, f, st) : product<LAST>(P, xt, p.M, p.N, p.M, batch, f, st);
+            const hipError_t e = tall ? product<LAST>(p, xt, P, p.N, p.M, p.M, batch, f, st) : product<LAST>(p, P, xt, p.M, p.N, p.M, batch, f, st);
             if (e != hipSuccess) return e;
         }
         U = next;
