@@ -16,6 +16,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "sage_internal.h"
 
@@ -146,34 +147,114 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
     j = t - (int)((int64_t)i * (i + 1) / 2);
 }
 
+// Rows r .. r + 3 of column c of a product, sums as they are: scaled, and written in the product's form. mirror: the tile is off the diagonal.
+template <int MODE>
+__device__ __forceinline__ void finish(const Finish& fin, int64_t b, int64_t r, int64_t c, bool mirror, f32x4 sum) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = sum[e] * fin.f;
+    if constexpr (MODE == LAST) {
+        if (c < fin.cols) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (r + e < fin.rows) {
+                    const int64_t o = b * fin.stride_out + (r + e) * fin.ld_out + c;
+                    if (fin.out16) ((uint16_t*)fin.out)[o] = narrow<uint16_t>(v[e]);
+                    else ((float*)fin.out)[o] = v[e];
+                }
+        }
+    } else {
+        const int64_t at_c = (c >> 5) * 64 + (c & 31), at_r = (r >> 5) * 64 + (r & 31);
+        if constexpr (MODE == POLY) {
+            const f16* ap = fin.A.p + b * fin.A.batch + r * fin.A.pitch + at_c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(fin.fa, (float)ap[e * fin.A.pitch] + (float)ap[e * fin.A.pitch + 32], v[e]);
+        }
+        if constexpr (MODE == GRAM || MODE == POLY) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (r + e == c) v[e] += fin.diag;
+        }
+        f16x4 hi, lo;
+        f16* cp = fin.C.p + b * fin.C.batch + r * fin.C.pitch + at_c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f16 x, y;
+            split(v[e], x, y);
+            hi[e] = x;
+            lo[e] = y;
+            cp[e * fin.C.pitch] = x;
+            cp[e * fin.C.pitch + 32] = y;
+        }
+        // the same values the other way round; a diagonal tile has its own mirror image in it
+        if (MODE == STEP || mirror) {
+            const Parts& t = MODE == STEP ? fin.Ct : fin.C;
+            f16* tp = t.p + b * t.batch + c * t.pitch + at_r;
+            *(f16x4*)tp = hi;
+            *(f16x4*)(tp + 32) = lo;
+        }
+    }
+}
+
 constexpr int wait_for_loads(int left) { return (left & 15) | (left >> 4) << 14 | 0x0F70; }  // until so many are on their way
+
+// The place of a work-group's tile. Work-groups i and i + 8 run on one XCD and share its L2: each XCD gets a run of consecutive tiles, and
+// consecutive tiles go down groups of 8 rows of tiles, column by column, so that those at work together use few rows of either
+// factor (nothing but the time depends on it).
+__device__ __forceinline__ int tile_in_turn(int block, int blocks) {
+    const int x = block & 7, each = blocks >> 3, more = blocks & 7;
+    return x * each + min(x, more) + (block >> 3);
+}
+template <bool SYM>
+__device__ __forceinline__ void tile_place(int at, int tiles_r, int tiles_c, int& ti, int& tj) {
+    if constexpr (SYM) {  // groups of 8 rows of a lower triangle: 8 g columns of 8, then a triangle of 8; 32 g^2 + 4 g before group g
+        int g = (int)((sqrtf(128.f * (float)at + 16.f) - 4.f) * (1.f / 64.f));
+        while (32 * g * g + 4 * g > at) --g;
+        while (32 * (g + 1) * (g + 1) + 4 * (g + 1) <= at) ++g;
+        const int in = at - (32 * g * g + 4 * g), rows = min(8, tiles_r - 8 * g);
+        if (in < 8 * g * rows) {
+            ti = 8 * g + in % rows;
+            tj = in / rows;
+        } else {
+            triangle(in - 8 * g * rows, ti, tj);
+            ti += 8 * g;
+            tj += 8 * g;
+        }
+    } else {
+        const int g = at / (8 * tiles_c), in = at - g * 8 * tiles_c, rows = min(8, tiles_r - 8 * g);
+        ti = 8 * g + in % rows;
+        tj = in / rows;
+    }
+}
 
 // C = A B^T of padded matrices in parts, both along the summed index: tiles of 32 WR RB x 32 WC CB, WR x WC waves with RB x CB
 // instruction tiles of 32 x 32 each. Blocks of 32 of the summed index go straight to LDS, NST - 1 on their way while one is multiplied; a row's
 // eight pieces of 16 bytes are stored in an order turned by the row's number, so that the reads of eight rows meet
 // different banks. (The loads deposit in lane order: it is their addresses that are turned.) KS > 1: as many such groups of waves take the
 // blocks of the summed index in turn, and the first adds up what they have: a tile alone on a CU waits for its own loads and LDS
-// reads most of the time.
+// reads most of the time. splits > 1: as many work-groups have a tile, each a part of the summed index, and leave their sums to
+// ortho_join_kernel.
 template <int WR, int WC, int RB, int CB, int KS, int NST, int MODE>
-__global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin) {
+__global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin,
+                                                                               int splits, f32x4* __restrict__ partial) {
     constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, THREADS = WR * WC * 64;
     constexpr int STAGE = (TM + TN) * 8;  // pieces of 16 bytes
     constexpr int LOADS = STAGE / THREADS;
     static_assert(STAGE % THREADS == 0 && TM * 8 % THREADS == 0, "whole loads");
-    static_assert(LOADS * (NST - 2) < 64, "a wait counts up to 63");
+    static_assert(LOADS * (NST - 1) < 64, "a wait counts up to 63");
     static_assert(KS == 1 || (KS - 1) * RB * CB * 4 * THREADS <= KS * NST * STAGE, "room for the sums");
     extern __shared__ u32x4 lds[];  // KS * NST * STAGE
     constexpr bool SYM = MODE == GRAM || MODE == POLY;
     const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
-    const int64_t b = blockIdx.x / per;
-    const int at = blockIdx.x % per;
+    constexpr bool SPLIT = RB == 2 && KS == 1;
+    const int unit = tile_in_turn(blockIdx.x, gridDim.x);
+    const int tile = SPLIT ? unit / splits : unit, part = SPLIT ? unit % splits : 0;
+    const int64_t b = tile / per;
+    const int at = tile % per;
+    const int first = SPLIT ? kblocks * part / splits : 0;
+    if (SPLIT) kblocks = kblocks * (part + 1) / splits - first;
     int ti, tj;
-    if constexpr (SYM) {
-        triangle(at, ti, tj);
-    } else {
-        ti = at / tiles_c;
-        tj = at % tiles_c;
-    }
+    tile_place<SYM>(at, tiles_r, tiles_c, ti, tj);
     const int group = KS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
     const int tid = threadIdx.x - group * THREADS, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -191,7 +272,7 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
     auto stage = [&](int kb, int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int q = 0; q < LOADS; ++q)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[q] + (int64_t)kb * 64),
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[q] + (int64_t)(first + kb) * 64),
                                              (__attribute__((address_space(3))) void*)(ring + buf * STAGE + q * THREADS + wave * 64), 16, 0, 0);
     };
 
@@ -203,48 +284,58 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    // (beyond the end the last block is loaded again and not used, so that every turn waits for the same number of loads)
-#pragma unroll
-    for (int i = 0; i < NST - 1; ++i) stage(min(i * KS + group, kblocks - 1), i);
+    // Factors of half a block: 16 of the summed index
+    struct Factors {
+        f16x8 a[RB][2], c[CB][2];
+    };
     const int arow = wr * 32 * RB + l32, brow = TM + wc * 32 * CB + l32;
-    int buf = 0;
-    for (int kb = group; kb < kblocks + group; kb += KS) {
-        // this block has landed; everyone is done with the buffer of the one before
+    auto read = [&](Factors& f, int buf, int s) __attribute__((always_inline)) {
+        const u32x4* st = ring + buf * STAGE;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int piece = (4 * p + 2 * s + h) ^ (l32 & 7);
+#pragma unroll
+            for (int i = 0; i < RB; ++i) f.a[i][p] = __builtin_bit_cast(f16x8, st[(arow + 32 * i) * 8 + piece]);
+#pragma unroll
+            for (int j = 0; j < CB; ++j) f.c[j][p] = __builtin_bit_cast(f16x8, st[(brow + 32 * j) * 8 + piece]);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (the scheduler would put each read next to its use, which then waits for it)
+    };
+    auto multiply = [&](const Factors& f) __attribute__((always_inline)) {
+        constexpr int PA[3] = {1, 0, 0}, PC[3] = {0, 1, 0};
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.a[i][PA[p]], f.c[j][PC[p]], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // NST blocks are on their way before the first is used. (Beyond the end the last block is loaded again and not used, so that every turn
+    // waits for the same number of loads.)
+#pragma unroll
+    for (int i = 0; i < NST; ++i) stage(min(i * KS + group, kblocks - 1), i);
+    auto meet = [&](auto wait) __attribute__((always_inline)) {  // the next block has landed; everyone has read the one before it
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(wait_for_loads(LOADS * (NST - 2)));
+        __builtin_amdgcn_s_waitcnt(decltype(wait)::value);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        stage(min(kb + (NST - 1) * KS, kblocks - 1), buf == 0 ? NST - 1 : buf - 1);
-        const u32x4* st = ring + buf * STAGE;
+    };
+    Factors f0, f1;
+    meet(std::integral_constant<int, wait_for_loads(LOADS * (NST - 1))>{});
+    read(f0, 0, 0);
+    int buf = 0;
+    for (int kb = group; kb < kblocks + group; kb += KS) {
+        const bool some = KS == 1 || kb < kblocks;  // (the last turn has blocks for some groups only)
+        read(f1, buf, 1);
+        if (some) multiply(f0);
+        meet(std::integral_constant<int, wait_for_loads(LOADS * (NST - 2)) & ~0x0F00>{});  // (and nothing of this block is still being read from LDS)
+        stage(min(kb + NST * KS, kblocks - 1), buf);
         buf = buf == NST - 1 ? 0 : buf + 1;
-        if (KS > 1 && kb >= kblocks) continue;  // (the last turn has blocks for some groups only)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            f16x8 a[RB][2], c[CB][2];
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const int piece = (4 * p + 2 * s + h) ^ (l32 & 7);
-#pragma unroll
-                for (int i = 0; i < RB; ++i) a[i][p] = __builtin_bit_cast(f16x8, st[(arow + 32 * i) * 8 + piece]);
-#pragma unroll
-                for (int j = 0; j < CB; ++j) c[j][p] = __builtin_bit_cast(f16x8, st[(brow + 32 * j) * 8 + piece]);
-            }
-#pragma unroll
-            for (int i = 0; i < RB; ++i)
-#pragma unroll
-                for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][1], c[j][0], acc[i][j], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < RB; ++i)
-#pragma unroll
-                for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], c[j][1], acc[i][j], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < RB; ++i)
-#pragma unroll
-                for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], c[j][0], acc[i][j], 0, 0, 0);
-        }
+        read(f0, buf, 0);
+        if (some) multiply(f1);
     }
-
     __builtin_amdgcn_s_waitcnt(wait_for_loads(0));  // nothing on its way to LDS when the work-group ends or uses it otherwise
     if constexpr (KS > 1) {
         f32x4* sums = (f32x4*)lds;
@@ -275,61 +366,151 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
                     }
     }
 
+    if (SPLIT && splits > 1) {
+        // the sums of this part of the summed index, in the threads' own order
+        f32x4* to = partial + ((int64_t)unit * RB * CB * 4) * THREADS + tid;
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int j = 0; j < CB; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    to[((i * CB + j) * 4 + g) * THREADS] = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        return;
+    }
     // A lane has four consecutive rows of one column: entries 4 g .. 4 g + 3 are rows 8 g + 4 h + 0 .. 3.
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
         for (int j = 0; j < CB; ++j)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int64_t r = (int64_t)ti * TM + (wr * RB + i) * 32 + 8 * g + 4 * h;
-                const int64_t c = (int64_t)tj * TN + (wc * CB + j) * 32 + l32;
-                float v[4];
+            for (int g = 0; g < 4; ++g)
+                finish<MODE>(fin, b, (int64_t)ti * TM + (wr * RB + i) * 32 + 8 * g + 4 * h, (int64_t)tj * TN + (wc * CB + j) * 32 + l32, ti != tj,
+                             f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+}
+
+// The same for few tiles: 64 x 64, all of it by each of four waves, which take the blocks of the summed index in turn and add up what
+// they have in the end. A wave has its own ring of two blocks and waits for nobody. (Four waves with a quarter of the tile each read
+// twice as much from LDS as the matrix cores can use: 1000 x 2049, A 21 us with them and XX so.)
+template <int MODE>
+__global__ __launch_bounds__(256) void ortho_wave_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin) {
+    constexpr int STAGE = 128 * 8, LOADS = 16, KS = 4;
+    extern __shared__ u32x4 lds[];  // KS * 2 * STAGE
+    constexpr bool SYM = MODE == GRAM || MODE == POLY;
+    const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
+    const int tile = tile_in_turn(blockIdx.x, gridDim.x), at = tile % per;
+    const int64_t b = tile / per;
+    int ti, tj;
+    tile_place<SYM>(at, tiles_r, tiles_c, ti, tj);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, h = lane >> 5;
+    u32x4* const ring = lds + wave * 2 * STAGE;
+    const f16* abase = A.p + b * A.batch + (int64_t)ti * 64 * A.pitch;
+    const f16* bbase = B.p + b * B.batch + (int64_t)tj * 64 * B.pitch;
+    const int turned = ((lane & 7) ^ (lane >> 3)) * 8;
+    const uint32_t aoff = (uint32_t)((lane >> 3) * A.pitch) + turned, boff = (uint32_t)((lane >> 3) * B.pitch) + turned;
+    auto stage = [&](int kb, int buf) __attribute__((always_inline)) {
+        const int64_t at_k = (int64_t)min(kb, kblocks - 1) * 64;  // (beyond the end the last block again, not used)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e] * fin.f;
-                if constexpr (MODE == LAST) {
-                    if (c < fin.cols) {
+        for (int q = 0; q < LOADS; ++q) {
+            const f16* from = q < 8 ? abase + (int64_t)(q * 8) * A.pitch + at_k : bbase + (int64_t)(q * 8 - 64) * B.pitch + at_k;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (q < 8 ? aoff : boff)),
+                                             (__attribute__((address_space(3))) void*)(ring + buf * STAGE + q * 64), 16, 0, 0);
+        }
+    };
+    f32x16 acc[2][2];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (r + e < fin.rows) {
-                                const int64_t o = b * fin.stride_out + (r + e) * fin.ld_out + c;
-                                if (fin.out16) ((uint16_t*)fin.out)[o] = narrow<uint16_t>(v[e]);
-                                else ((float*)fin.out)[o] = v[e];
-                            }
-                    }
-                } else {
-                    const int64_t at_c = (c >> 5) * 64 + (c & 31), at_r = (r >> 5) * 64 + (r & 31);
-                    if constexpr (MODE == POLY) {
-                        const f16* ap = fin.A.p + b * fin.A.batch + r * fin.A.pitch + at_c;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            v[e] = fmaf(fin.fa, (float)ap[e * fin.A.pitch] + (float)ap[e * fin.A.pitch + 32], v[e]);
-                    }
-                    if constexpr (SYM) {
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (r + e == c) v[e] += fin.diag;
-                    }
-                    f16x4 hi, lo;
-                    f16* cp = fin.C.p + b * fin.C.batch + r * fin.C.pitch + at_c;
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    struct Factors {
+        f16x8 a[2][2], c[2][2];
+    };
+    auto read = [&](Factors& f, int buf, int s) __attribute__((always_inline)) {
+        const u32x4* st = ring + buf * STAGE + l32 * 8;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        f16 x, y;
-                        split(v[e], x, y);
-                        hi[e] = x;
-                        lo[e] = y;
-                        cp[e * fin.C.pitch] = x;
-                        cp[e * fin.C.pitch + 32] = y;
-                    }
-                    // the same values the other way round; a diagonal tile has its own mirror image in it
-                    if (MODE == STEP || ti != tj) {
-                        const Parts& t = MODE == STEP ? fin.Ct : fin.C;
-                        f16* tp = t.p + b * t.batch + c * t.pitch + at_r;
-                        *(f16x4*)tp = hi;
-                        *(f16x4*)(tp + 32) = lo;
-                    }
-                }
-            }
+        for (int p = 0; p < 2; ++p) {
+            const int piece = (4 * p + 2 * s + h) ^ (l32 & 7);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) f.a[i][p] = __builtin_bit_cast(f16x8, st[32 * i * 8 + piece]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) f.c[j][p] = __builtin_bit_cast(f16x8, st[(64 + 32 * j) * 8 + piece]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](const Factors& f) __attribute__((always_inline)) {
+        constexpr int PA[3] = {1, 0, 0}, PC[3] = {0, 1, 0};
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.a[i][PA[p]], f.c[j][PC[p]], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto wait = [&](auto imm) __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(decltype(imm)::value);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    using std::integral_constant;
+    Factors f0, f1;
+    stage(wave, 0);
+    stage(wave + KS, 1);
+    wait(integral_constant<int, wait_for_loads(LOADS)>{});
+    read(f0, 0, 0);
+    int buf = 0;
+    for (int kb = wave; kb < kblocks; kb += KS) {
+        read(f1, buf, 1);
+        multiply(f0);
+        wait(integral_constant<int, wait_for_loads(63) & ~0x0F00>{});  // this block has been read from LDS
+        stage(kb + 2 * KS, buf);
+        wait(integral_constant<int, wait_for_loads(LOADS)>{});  // the next one is there
+        buf ^= 1;
+        read(f0, buf, 0);
+        multiply(f1);
+    }
+    wait(integral_constant<int, wait_for_loads(0) & ~0x0F00>{});  // nothing on its way to or from LDS
+    __syncthreads();
+    f32x4* sums = (f32x4*)lds;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                sums[((wave * 4 + 2 * i + j) * 4 + g) * 64 + lane] = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    __syncthreads();
+    const int i = wave >> 1, j = wave & 1;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        f32x4 v = sums[(wave * 4 + g) * 64 + lane];
+#pragma unroll
+        for (int q = 1; q < KS; ++q) v += sums[((q * 4 + wave) * 4 + g) * 64 + lane];
+        finish<MODE>(fin, b, (int64_t)ti * 64 + i * 32 + 8 * g + 4 * h, (int64_t)tj * 64 + j * 32 + l32, ti != tj, v);
+    }
+}
+
+// The sums of the parts added up, in their order, and finished: a work-group has the 4 KB that 256 threads wrote together.
+template <int WR, int WC, int RB, int CB, int MODE>
+__global__ __launch_bounds__(WR * WC * 64) void ortho_join_kernel(const f32x4* __restrict__ partial, int splits, int tiles_r, int tiles_c, Finish fin) {
+    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, THREADS = WR * WC * 64, PIECES = RB * CB * 4;
+    constexpr bool SYM = MODE == GRAM || MODE == POLY;
+    const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
+    const int piece = blockIdx.x % PIECES, tile = blockIdx.x / PIECES, at = tile % per;
+    const int64_t b = tile / per;
+    int ti, tj;
+    tile_place<SYM>(at, tiles_r, tiles_c, ti, tj);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, h = lane >> 5;
+    const int wr = wave / WC, wc = wave % WC, i = piece / 4 / CB, j = piece / 4 % CB, g = piece % 4;
+    const f32x4* from = partial + ((int64_t)tile * splits * PIECES + piece) * THREADS + tid;
+    f32x4 v = from[0];
+    for (int q = 1; q < splits; ++q) v += from[(int64_t)q * PIECES * THREADS];
+    finish<MODE>(fin, b, (int64_t)ti * TM + (wr * RB + i) * 32 + 8 * g + 4 * h, (int64_t)tj * TN + (wc * CB + j) * 32 + l32, ti != tj, v);
 }
 
 // ---- the plan ---------------------------------------------------------------------------------------------------
@@ -350,20 +531,27 @@ struct Plan {
     int64_t x, a;        // halves of X (either way) and of A
     int64_t per;         // bytes of one matrix
     int64_t chunk;       // matrices at a time
+    int64_t bytes;       // of the work space
 };
 
 int64_t padded(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
 // tiles of 128 x 128 of X, from which on they are used
-constexpr int64_t BIG_FROM = 256;
+constexpr int64_t BIG_FROM = 64;
+constexpr int64_t TWO_EACH = 400;  // tiles from which on a CU has two work-groups, with shorter rings
+constexpr int64_t ONE_EACH = 256;  // work-groups that one tile each, or a part of one, is cut into at most
+constexpr int64_t JOIN_BYTES = ONE_EACH * 128 * 128 * 4;
+
+// Parts of the summed index for so many tiles: no more work-groups than CUs, of no less than 8 blocks each.
+int splits_of(int64_t tiles, int64_t k) { return (int)std::max<int64_t>(1, std::min<int64_t>(ONE_EACH / tiles, k / KB / 8)); }
 
 Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     Plan p;
     p.m = std::min(rows, cols);
     p.n = std::max(rows, cols);
     const int64_t tiles = (p.m + 127) / 128 * ((p.n + 127) / 128) * batch;
-    p.big = tiles >= BIG_FROM;
+    p.big = p.m > 64 && tiles >= BIG_FROM;  // (a side of up to 64 would be padded to twice that and more)
     p.M = padded(p.m, p.big ? 128 : 64);
     p.N = padded(p.n, p.big ? 128 : 64);
     p.groups = (int)std::min<int64_t>(rows, std::max<int64_t>(1, std::min<int64_t>(256, rows * cols / 4096)));
@@ -371,6 +559,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     p.a = 2 * p.M * p.M;
     p.per = (3 * p.x + 2 * p.a) * 2 + align256(8 * p.groups);
     p.chunk = std::max<int64_t>(1, std::min(batch, WORK_LIMIT / p.per));
+    p.bytes = p.per * p.chunk + (p.big ? JOIN_BYTES : 0);
     return p;
 }
 
@@ -404,22 +593,31 @@ double scale_for(double top) {
 }
 
 template <int MODE, int RB, int KS, int NST>
-hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, hipStream_t st) {
+hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, int splits,
+                      f32x4* partial, hipStream_t st) {
     constexpr int WR = 2, WC = 2, CB = RB;
     constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, BYTES = KS * NST * (TM + TN) * 128;
     const auto kernel = ortho_product_kernel<WR, WC, RB, CB, KS, NST, MODE>;
     if (hipError_t e = ensure_dynamic_lds((const void*)kernel, BYTES); e != hipSuccess) return e;
     const int tr = (int)(rows / TM), tc = (int)(cols / TN);
-    kernel<<<dim3((unsigned)(tiles_of<MODE>(rows, cols, TM) * batch)), KS * WR * WC * 64, BYTES, st>>>(A, B, (int)(k / KB), tr, tc, fin);
+    const unsigned tiles = (unsigned)(tiles_of<MODE>(rows, cols, TM) * batch);
+    kernel<<<dim3(tiles * splits), KS * WR * WC * 64, BYTES, st>>>(A, B, (int)(k / KB), tr, tc, fin, splits, partial);
+    if (splits > 1) ortho_join_kernel<WR, WC, RB, CB, MODE><<<dim3(tiles * RB * CB * 4), WR * WC * 64, 0, st>>>(partial, splits, tr, tc, fin);
     return hipGetLastError();
 }
 
 template <int MODE>
 hipError_t product(const Plan& p, const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin,
-                   hipStream_t st) {
-    if (p.big && tiles_of<MODE>(rows, cols, 128) * batch >= BIG_FROM) return product_of<MODE, 2, 1, 2>(A, B, rows, cols, k, batch, fin, st);
-    if (tiles_of<MODE>(rows, cols, 64) * batch <= 256 && k >= 8 * KB) return product_of<MODE, 1, 4, 2>(A, B, rows, cols, k, batch, fin, st);
-    return product_of<MODE, 1, 1, 3>(A, B, rows, cols, k, batch, fin, st);
+                   f32x4* partial, hipStream_t st) {
+    if (p.big) {
+        const int64_t tiles = tiles_of<MODE>(rows, cols, 128) * batch;
+        if (tiles >= TWO_EACH) return product_of<MODE, 2, 1, 2>(A, B, rows, cols, k, batch, fin, 1, nullptr, st);
+        return product_of<MODE, 2, 1, 4>(A, B, rows, cols, k, batch, fin, splits_of(tiles, k), partial, st);
+    }
+    const auto kernel = ortho_wave_kernel<MODE>;
+    if (hipError_t e = ensure_dynamic_lds((const void*)kernel, 131072); e != hipSuccess) return e;
+    kernel<<<dim3((unsigned)(tiles_of<MODE>(rows, cols, 64) * batch)), 256, 131072, st>>>(A, B, (int)(k / KB), (int)(rows / 64), (int)(cols / 64), fin);
+    return hipGetLastError();
 }
 
 template <class T>
@@ -432,6 +630,7 @@ hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t c
     w += 3 * c * p.x;
     const Parts A{w, 2 * p.M, p.a}, P{w + c * p.a, 2 * p.M, p.a};
     double* partial = (double*)(w + 2 * c * p.a);
+    f32x4* const join = (f32x4*)(work + c * p.per);
 
     ortho_norm_kernel<T><<<dim3((unsigned)(p.groups * batch)), NORM_THREADS, 0, st>>>(G, rows, cols, ld, stride, partial, p.groups);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -449,25 +648,25 @@ hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t c
         if (cc != 0.0) {
             f.f = (float)(sa / (sx * sx));
             f.C = A;
-            if (hipError_t e = product<GRAM>(p, X, X, p.M, p.M, p.N, batch, f, st); e != hipSuccess) return e;
+            if (hipError_t e = product<GRAM>(p, X, X, p.M, p.M, p.N, batch, f, join, st); e != hipSuccess) return e;
             f.f = (float)(cc * sp / (sa * sa));
             f.fa = (float)(cb * sp / sa);
             f.diag = (float)(ca * sp);
             f.A = A;
             f.C = P;
-            if (hipError_t e = product<POLY>(p, A, A, p.M, p.M, p.M, batch, f, st); e != hipSuccess) return e;
+            if (hipError_t e = product<POLY>(p, A, A, p.M, p.M, p.M, batch, f, join, st); e != hipSuccess) return e;
         } else {
             f.f = (float)(cb * sp / (sx * sx));
             f.diag = (float)(ca * sp);
             f.C = P;
-            if (hipError_t e = product<GRAM>(p, X, X, p.M, p.M, p.N, batch, f, st); e != hipSuccess) return e;
+            if (hipError_t e = product<GRAM>(p, X, X, p.M, p.M, p.N, batch, f, join, st); e != hipSuccess) return e;
         }
         const Parts& xt = Xt[s & 1];
         if (s + 1 < steps) {
             f.f = (float)(sn / (sp * sx));
             f.C = X;
             f.Ct = Xt[(s + 1) & 1];
-            if (hipError_t e = product<STEP>(p, P, xt, p.M, p.N, p.M, batch, f, st); e != hipSuccess) return e;
+            if (hipError_t e = product<STEP>(p, P, xt, p.M, p.N, p.M, batch, f, join, st); e != hipSuccess) return e;
         } else {
             f.f = (float)(scale / (sp * sx));
             f.out = out;
@@ -476,7 +675,7 @@ hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t c
             f.rows = rows;
             f.cols = cols;
             f.out16 = sizeof(T) == 2;
-            const hipError_t e = tall ? product<LAST>(p, xt, P, p.N, p.M, p.M, batch, f, st) : product<LAST>(p, P, xt, p.M, p.N, p.M, batch, f, st);
+            const hipError_t e = tall ? product<LAST>(p, xt, P, p.N, p.M, p.M, batch, f, join, st) : product<LAST>(p, P, xt, p.M, p.N, p.M, batch, f, join, st);
             if (e != hipSuccess) return e;
         }
         U = next;
@@ -503,7 +702,7 @@ bool layout_ok(const void* p, int dtype, int64_t batch, int64_t rows, int64_t co
 extern "C" int sage_orthogonalize_work(sage_dtype dtype, int64_t batch, int64_t rows, int64_t cols, size_t* bytes) {
     if (!bytes || !sage::sizes_ok(dtype, batch, rows, cols)) return SAGE_ERR_ARG;
     const sage::Plan p = sage::plan_of(batch, rows, cols);
-    *bytes = batch ? (size_t)(p.per * p.chunk) : 0;
+    *bytes = batch ? (size_t)p.bytes : 0;
     return SAGE_OK;
 }
 
@@ -532,7 +731,7 @@ extern "C" int sage_orthogonalize(const void* G, sage_dtype dtype, int64_t batch
         if (g0 < o1 && o0 < g1) return SAGE_ERR_ARG;
     }
     const Plan p = plan_of(batch, rows, cols);
-    if (!work || (uintptr_t)work % 256 || work_bytes < (size_t)(p.per * p.chunk)) return SAGE_ERR_ARG;
+    if (!work || (uintptr_t)work % 256 || work_bytes < (size_t)p.bytes) return SAGE_ERR_ARG;
     for (int64_t b = 0; b < batch; b += p.chunk) {
         const int64_t n = std::min(p.chunk, batch - b);
         const hipError_t e =
