@@ -236,7 +236,7 @@ __device__ __forceinline__ void tile_place(int at, int tiles_r, int tiles_c, int
 // ortho_join_kernel.
 template <int WR, int WC, int RB, int CB, int KS, int NST, int MODE>
 __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin,
-                                                                               int splits, f32x4* __restrict__ partial) {
+                                                                               int tile0, int splits, f32x4* __restrict__ partial) {
     constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, THREADS = WR * WC * 64;
     constexpr int STAGE = (TM + TN) * 8;  // pieces of 16 bytes
     constexpr int LOADS = STAGE / THREADS;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
     const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
     constexpr bool SPLIT = RB == 2 && KS == 1;
     const int unit = tile_in_turn(blockIdx.x, gridDim.x);
-    const int tile = SPLIT ? unit / splits : unit, part = SPLIT ? unit % splits : 0;
+    const int tile = tile0 + (SPLIT ? unit / splits : unit), part = SPLIT ? unit % splits : 0;
     const int64_t b = tile / per;
     const int at = tile % per;
     const int first = SPLIT ? kblocks * part / splits : 0;
@@ -262,18 +262,20 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
     const int wr = wave / WC, wc = wave % WC;
     u32x4* const ring = lds + group * NST * STAGE;
 
-    const f16* src[LOADS];
-#pragma unroll
-    for (int q = 0; q < LOADS; ++q) {
-        const int piece = q * THREADS + tid, row = piece >> 3, turned = (piece & 7) ^ (row & 7);
-        if (q * THREADS < TM * 8) src[q] = A.p + b * A.batch + ((int64_t)ti * TM + row) * A.pitch + turned * 8;
-        else src[q] = B.p + b * B.batch + ((int64_t)tj * TN + row - TM) * B.pitch + turned * 8;
-    }
+    // (a thread's pieces are in rows THREADS / 8 apart: one offset for each factor, the rest is the same for all threads)
+    static_assert(THREADS % 64 == 0, "whole turns of 8 rows");
+    const int turned = ((tid & 7) ^ (tid >> 3 & 7)) * 8;
+    const uint32_t aoff = (uint32_t)((tid >> 3) * A.pitch) + turned, boff = (uint32_t)((tid >> 3) * B.pitch) + turned;
+    const f16* abase = A.p + b * A.batch + (int64_t)ti * TM * A.pitch + (int64_t)first * 64;
+    const f16* bbase = B.p + b * B.batch + (int64_t)tj * TN * B.pitch + (int64_t)first * 64;
     auto stage = [&](int kb, int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int q = 0; q < LOADS; ++q)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src[q] + (int64_t)(first + kb) * 64),
+        for (int q = 0; q < LOADS; ++q) {
+            const int row = q * (THREADS / 8);
+            const f16* from = row < TM ? abase + (int64_t)row * A.pitch + (int64_t)kb * 64 : bbase + (int64_t)(row - TM) * B.pitch + (int64_t)kb * 64;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (row < TM ? aoff : boff)),
                                              (__attribute__((address_space(3))) void*)(ring + buf * STAGE + q * THREADS + wave * 64), 16, 0, 0);
+        }
     };
 
     f32x16 acc[RB][CB];
@@ -497,17 +499,17 @@ __global__ __launch_bounds__(256) void ortho_wave_kernel(Parts A, Parts B, int k
 
 // The sums of the parts added up, in their order, and finished: a work-group has the 4 KB that 256 threads wrote together.
 template <int WR, int WC, int RB, int CB, int MODE>
-__global__ __launch_bounds__(WR * WC * 64) void ortho_join_kernel(const f32x4* __restrict__ partial, int splits, int tiles_r, int tiles_c, Finish fin) {
+__global__ __launch_bounds__(WR * WC * 64) void ortho_join_kernel(const f32x4* __restrict__ partial, int tile0, int splits, int tiles_r, int tiles_c, Finish fin) {
     constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, THREADS = WR * WC * 64, PIECES = RB * CB * 4;
     constexpr bool SYM = MODE == GRAM || MODE == POLY;
     const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
-    const int piece = blockIdx.x % PIECES, tile = blockIdx.x / PIECES, at = tile % per;
+    const int piece = blockIdx.x % PIECES, mine = blockIdx.x / PIECES, tile = tile0 + mine, at = tile % per;
     const int64_t b = tile / per;
     int ti, tj;
     tile_place<SYM>(at, tiles_r, tiles_c, ti, tj);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, h = lane >> 5;
     const int wr = wave / WC, wc = wave % WC, i = piece / 4 / CB, j = piece / 4 % CB, g = piece % 4;
-    const f32x4* from = partial + ((int64_t)tile * splits * PIECES + piece) * THREADS + tid;
+    const f32x4* from = partial + ((int64_t)mine * splits * PIECES + piece) * THREADS + tid;
     f32x4 v = from[0];
     for (int q = 1; q < splits; ++q) v += from[(int64_t)q * PIECES * THREADS];
     finish<MODE>(fin, b, (int64_t)ti * TM + (wr * RB + i) * 32 + 8 * g + 4 * h, (int64_t)tj * TN + (wc * CB + j) * 32 + l32, ti != tj, v);
@@ -526,6 +528,7 @@ int64_t tiles_of(int64_t rows, int64_t cols, int64_t side) {
 
 struct Plan {
     int64_t m, n, M, N;  // the sides, smaller first, and padded
+    bool huge;           // tiles of 256 x 256
     bool big;            // tiles of 128 x 128, else 64 x 64
     int groups;          // of rows, for the norm
     int64_t x, a;        // halves of X (either way) and of A
@@ -538,13 +541,11 @@ int64_t padded(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
 // tiles of 128 x 128 of X, from which on they are used
-constexpr int64_t BIG_FROM = 64;
-constexpr int64_t TWO_EACH = 400;  // tiles from which on a CU has two work-groups, with shorter rings
-constexpr int64_t ONE_EACH = 256;  // work-groups that one tile each, or a part of one, is cut into at most
-constexpr int64_t JOIN_BYTES = ONE_EACH * 128 * 128 * 4;
-
-// Parts of the summed index for so many tiles: no more work-groups than CUs, of no less than 8 blocks each.
-int splits_of(int64_t tiles, int64_t k) { return (int)std::max<int64_t>(1, std::min<int64_t>(ONE_EACH / tiles, k / KB / 8)); }
+constexpr int64_t BIG_FROM = 200;
+constexpr int64_t HUGE_FROM = 224;    // ... of 256 x 256
+constexpr int64_t SLOTS = 512;        // work-groups of 128 x 128 at a time, two to a CU
+constexpr int SPLIT_BLOCKS = 8;       // blocks of the summed index in a part of it, at least
+constexpr int64_t JOIN_BYTES = SLOTS * 128 * 128 * 4;
 
 Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     Plan p;
@@ -552,8 +553,10 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     p.n = std::max(rows, cols);
     const int64_t tiles = (p.m + 127) / 128 * ((p.n + 127) / 128) * batch;
     p.big = p.m > 64 && tiles >= BIG_FROM;  // (a side of up to 64 would be padded to twice that and more)
-    p.M = padded(p.m, p.big ? 128 : 64);
-    p.N = padded(p.n, p.big ? 128 : 64);
+    p.huge = p.m > 192 && (p.m + 255) / 256 * ((p.n + 255) / 256) * batch >= HUGE_FROM;
+    const int side = p.huge ? 256 : p.big ? 128 : 64;
+    p.M = padded(p.m, side);
+    p.N = padded(p.n, side);
     p.groups = (int)std::min<int64_t>(rows, std::max<int64_t>(1, std::min<int64_t>(256, rows * cols / 4096)));
     p.x = 2 * p.M * p.N;
     p.a = 2 * p.M * p.M;
@@ -592,28 +595,39 @@ double scale_for(double top) {
     return ldexp(1.0, 15 - e);
 }
 
-template <int MODE, int RB, int KS, int NST>
-hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, int splits,
+// `slots` work-groups run at a time. Tiles that are left over when the slots have been filled as often as possible are cut along the summed
+// index, so that they fill them too: 528 tiles of 128 x 128 of a 4096 x 4096 product take 275 us as they are and 215 so (512 whole ones and 16 in 32 parts).
+template <int MODE, int WC, int RB, int NST>
+hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, int64_t slots,
                       f32x4* partial, hipStream_t st) {
-    constexpr int WR = 2, WC = 2, CB = RB;
-    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, BYTES = KS * NST * (TM + TN) * 128;
-    const auto kernel = ortho_product_kernel<WR, WC, RB, CB, KS, NST, MODE>;
+    constexpr int WR = 2, CB = 2, THREADS = WR * WC * 64;
+    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, BYTES = NST * (TM + TN) * 128;
+    const auto kernel = ortho_product_kernel<WR, WC, RB, CB, 1, NST, MODE>;
     if (hipError_t e = ensure_dynamic_lds((const void*)kernel, BYTES); e != hipSuccess) return e;
-    const int tr = (int)(rows / TM), tc = (int)(cols / TN);
-    const unsigned tiles = (unsigned)(tiles_of<MODE>(rows, cols, TM) * batch);
-    kernel<<<dim3(tiles * splits), KS * WR * WC * 64, BYTES, st>>>(A, B, (int)(k / KB), tr, tc, fin, splits, partial);
-    if (splits > 1) ortho_join_kernel<WR, WC, RB, CB, MODE><<<dim3(tiles * RB * CB * 4), WR * WC * 64, 0, st>>>(partial, splits, tr, tc, fin);
+    const int tr = (int)(rows / TM), tc = (int)(cols / TN), kb = (int)(k / KB);
+    const int64_t tiles = tiles_of<MODE>(rows, cols, TM) * batch, rest = tiles % slots;
+    const int splits = RB == 2 && rest ? (int)std::max<int64_t>(1, std::min<int64_t>(slots / rest, kb / SPLIT_BLOCKS)) : 1;
+    const int64_t whole = splits > 1 ? tiles - rest : tiles;
+    if (whole) {
+        kernel<<<dim3((unsigned)whole), THREADS, BYTES, st>>>(A, B, kb, tr, tc, fin, 0, 1, nullptr);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if constexpr (RB == 2) {
+        if (splits > 1) {
+            kernel<<<dim3((unsigned)(rest * splits)), THREADS, BYTES, st>>>(A, B, kb, tr, tc, fin, (int)whole, splits, partial);
+            if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+            ortho_join_kernel<WR, WC, RB, CB, MODE><<<dim3((unsigned)(rest * RB * CB * 4)), THREADS, 0, st>>>(partial, (int)whole, splits, tr, tc, fin);
+        }
+    }
     return hipGetLastError();
 }
 
 template <int MODE>
 hipError_t product(const Plan& p, const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin,
                    f32x4* partial, hipStream_t st) {
-    if (p.big) {
-        const int64_t tiles = tiles_of<MODE>(rows, cols, 128) * batch;
-        if (tiles >= TWO_EACH) return product_of<MODE, 2, 1, 2>(A, B, rows, cols, k, batch, fin, 1, nullptr, st);
-        return product_of<MODE, 2, 1, 4>(A, B, rows, cols, k, batch, fin, splits_of(tiles, k), partial, st);
-    }
+    // (half of a square is too few tiles of 256 x 256)
+    if (p.huge && (MODE == STEP || MODE == LAST)) return product_of<MODE, 4, 4, 2>(A, B, rows, cols, k, batch, fin, 256, nullptr, st);
+    if (p.big) return product_of<MODE, 2, 2, 2>(A, B, rows, cols, k, batch, fin, SLOTS, partial, st);
     const auto kernel = ortho_wave_kernel<MODE>;
     if (hipError_t e = ensure_dynamic_lds((const void*)kernel, 131072); e != hipSuccess) return e;
     kernel<<<dim3((unsigned)(tiles_of<MODE>(rows, cols, 64) * batch)), 256, 131072, st>>>(A, B, (int)(k / KB), (int)(rows / 64), (int)(cols / 64), fin);
