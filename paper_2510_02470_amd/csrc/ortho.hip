@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "logit_rows.h"
 #include "sage_internal.h"
 
 namespace sage {
@@ -28,7 +29,6 @@ typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int KB = 32;  // columns of a block of 128 bytes
 
@@ -46,41 +46,31 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
 
 // ---- X: the norm, and the matrix in parts both ways -------------------------------------------------------------
 
-template <class T>
-__device__ __forceinline__ float widen(T x) {
-    if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)x << 16);
-    else return x;
-}
-template <class T>
-__device__ __forceinline__ T narrow(float x) {
-    if constexpr (sizeof(T) == 2) {
-        const uint32_t u = __float_as_uint(x);
-        if (x != x) return (T)(u >> 16 | 0x40);
-        return (T)((u + 0x7FFF + (u >> 16 & 1)) >> 16);
-    } else {
-        return x;
-    }
-}
-
 constexpr int NORM_THREADS = 256;
 
-// Sums of squares of groups of rows, in fp64: any fp32 matrix has a norm there.
+// Sums of squares of groups of rows, in fp64: any fp32 matrix has a norm there. Bound by memory.
 template <class T>
 __global__ __launch_bounds__(NORM_THREADS) void ortho_norm_kernel(const T* __restrict__ G, int64_t rows, int64_t cols, int64_t ld,
                                                                   int64_t stride, double* __restrict__ partial, int groups) {
+    constexpr int VL = RowType<T>::VL;
     __shared__ double part[NORM_THREADS / 64];
     const int group = blockIdx.x % groups;
     const int64_t b = blockIdx.x / groups;
+    // a wave has a row at a time (short rows would leave most of a work-group without one)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     double s = 0.0;
-    for (int64_t r = group; r < rows; r += groups) {
+    for (int64_t r = (int64_t)group * 4 + wave; r < rows; r += 4 * groups) {
         const T* row = G + b * stride + r * ld;
-        for (int64_t t = threadIdx.x; t < cols; t += NORM_THREADS) {
-            const double x = widen(row[t]);
-            s = __builtin_fma(x, x, s);
+#pragma unroll 4
+        for (int64_t t = lane * VL; t < cols; t += 64 * VL) {
+            float x[VL];
+            row_floats(row, t, cols, 0.f, x);
+#pragma unroll
+            for (int i = 0; i < VL; ++i) s = __builtin_fma((double)x[i], (double)x[i], s);
         }
     }
     for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    if (lane == 0) part[wave] = s;
     __syncthreads();
     if (threadIdx.x == 0) partial[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
@@ -91,35 +81,47 @@ __global__ __launch_bounds__(256) void ortho_split_kernel(const T* __restrict__ 
                                                           const double* __restrict__ partial, int groups, double eps, double scale,
                                                           Parts R, Parts Q, int tiles_r, int tiles_c) {
     __shared__ float tile[64][65];
+    __shared__ double part[4];
     const int64_t b = blockIdx.x / (tiles_r * tiles_c);
     const int at = blockIdx.x % (tiles_r * tiles_c);
     const int64_t r0 = (int64_t)(at / tiles_c) * 64, c0 = (int64_t)(at % tiles_c) * 64;
-    __shared__ double part[4];
-    double s = (int)threadIdx.x < groups ? partial[b * groups + threadIdx.x] : 0.0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const T* g = G + b * stride;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int64_t r = r0 + wave + 4 * i, c = c0 + lane;
+        x[i] = r < rows && c < cols ? RowType<T>::widen(g[r * ld + c]) : 0.f;
+    }
+    double s = tid < groups ? partial[b * groups + tid] : 0.0;
     for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    if (lane == 0) part[wave] = s;
     __syncthreads();
     s = part[0] + part[1] + part[2] + part[3];
     const double inv = s > 0.0 || s != s ? scale / (sqrt(s) + eps) : 0.0;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const T* g = G + b * stride;
-    f16* rp = R.p + b * R.batch + (c0 >> 5) * 64 + (lane >> 5) * 64 + (lane & 31);
-    f16* qp = Q.p + b * Q.batch + (r0 >> 5) * 64 + (lane >> 5) * 64 + (lane & 31);
-    for (int i = wave; i < 64; i += 4) {
-        const int64_t r = r0 + i, c = c0 + lane;
-        const float v = r < rows && c < cols ? (float)((double)widen(g[r * ld + c]) * inv) : 0.f;
-        tile[i][lane] = v;
-        f16 hi, lo;
-        split(v, hi, lo);
-        rp[r * R.pitch] = hi;
-        rp[r * R.pitch + 32] = lo;
-    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) tile[wave + 4 * i][lane] = (float)((double)x[i] * inv);
     __syncthreads();
-    for (int i = wave; i < 64; i += 4) {
-        f16 hi, lo;
-        split(tile[lane][i], hi, lo);
-        qp[(c0 + i) * Q.pitch] = hi;
-        qp[(c0 + i) * Q.pitch + 32] = lo;
+    // eight entries of a row, then of a column, at a time: 16 bytes of high parts and 16 of low ones
+#pragma unroll
+    for (int way = 0; way < 2; ++way) {
+        const Parts& to = way ? Q : R;
+        const int64_t row0 = way ? c0 : r0, col0 = way ? r0 : c0;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int row = q * 32 + (tid >> 3), col = (tid & 7) * 8;
+            f16x8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                f16 u, v;
+                split(way ? tile[col + e][row] : tile[row][col + e], u, v);
+                hi[e] = u;
+                lo[e] = v;
+            }
+            f16* p = to.p + b * to.batch + (row0 + row) * to.pitch + (col0 + (col & 32)) * 2 + (col & 31);
+            *(f16x8*)p = hi;
+            *(f16x8*)(p + 32) = lo;
+        }
     }
 }
 
@@ -147,51 +149,81 @@ __device__ __forceinline__ void triangle(int t, int& i, int& j) {
     j = t - (int)((int64_t)i * (i + 1) / 2);
 }
 
-// Rows r .. r + 3 of column c of a product, sums as they are: scaled, and written in the product's form. mirror: the tile is off the diagonal.
+// 32 x 32 entries of a product from row r0 and column c0 on, by one wave: sums as they are (v[g][e]: row 8 g + 4 h + e of column l32, lane
+// l32 + 32 h), scaled, and written in the product's form. mirror: the tile is off the diagonal. lds: 4 KB of the wave's own, in which
+// the entries are put in the order of memory: whole lines of 128 bytes are stored.
 template <int MODE>
-__device__ __forceinline__ void finish(const Finish& fin, int64_t b, int64_t r, int64_t c, bool mirror, f32x4 sum) {
-    float v[4];
+__device__ __forceinline__ void finish(const Finish& fin, int64_t b, int64_t r0, int64_t c0, bool mirror, const f32x4* sum, f16* lds) {
+    const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    f32x4 v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = sum[e] * fin.f;
+    for (int g = 0; g < 4; ++g) v[g] = sum[g] * fin.f;
     if constexpr (MODE == LAST) {
+        const int64_t c = c0 + l32;
         if (c < fin.cols) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (r + e < fin.rows) {
-                    const int64_t o = b * fin.stride_out + (r + e) * fin.ld_out + c;
-                    if (fin.out16) ((uint16_t*)fin.out)[o] = narrow<uint16_t>(v[e]);
-                    else ((float*)fin.out)[o] = v[e];
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t r = r0 + 8 * g + 4 * h + e;
+                    if (r < fin.rows) {
+                        const int64_t o = b * fin.stride_out + r * fin.ld_out + c;
+                        if (fin.out16) ((uint16_t*)fin.out)[o] = RowType<uint16_t>::narrow(v[g][e]);
+                        else ((float*)fin.out)[o] = v[g][e];
+                    }
                 }
         }
     } else {
-        const int64_t at_c = (c >> 5) * 64 + (c & 31), at_r = (r >> 5) * 64 + (r & 31);
-        if constexpr (MODE == POLY) {
-            const f16* ap = fin.A.p + b * fin.A.batch + r * fin.A.pitch + at_c;
+        if constexpr (MODE == POLY) {  // A is symmetric: its entries at (c, r .. r + 3) are next to each other
+            const f16* ap = fin.A.p + b * fin.A.batch + (c0 + l32) * fin.A.pitch + r0 * 2 + 4 * h;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = fmaf(fin.fa, (float)ap[e * fin.A.pitch] + (float)ap[e * fin.A.pitch + 32], v[e]);
+            for (int g = 0; g < 4; ++g) {
+                const f16x4 hi = *(const f16x4*)(ap + 8 * g), lo = *(const f16x4*)(ap + 8 * g + 32);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[g][e] = fmaf(fin.fa, (float)hi[e] + (float)lo[e], v[g][e]);
+            }
         }
         if constexpr (MODE == GRAM || MODE == POLY) {
+            if (r0 == c0) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (r + e == c) v[e] += fin.diag;
-        }
-        f16x4 hi, lo;
-        f16* cp = fin.C.p + b * fin.C.batch + r * fin.C.pitch + at_c;
+                for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            f16 x, y;
-            split(v[e], x, y);
-            hi[e] = x;
-            lo[e] = y;
-            cp[e * fin.C.pitch] = x;
-            cp[e * fin.C.pitch + 32] = y;
+                    for (int e = 0; e < 4; ++e) v[g][e] += 8 * g + 4 * h + e == l32 ? fin.diag : 0.f;
+            }
         }
+        f16x4 hi[4], lo[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f16 x, y;
+                split(v[g][e], x, y);
+                hi[g][e] = x;
+                lo[g][e] = y;
+            }
+        // 16 bytes of a line at a time; where they lie in LDS is turned by the row, so that rows meet different banks
+        auto store = [&](const Parts& to, int64_t row, int64_t col) __attribute__((always_inline)) {
+            f16* p = to.p + b * to.batch + (row + (lane >> 3)) * to.pitch + col * 2 + (lane & 7) * 8;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) *(u32x4*)(p + (int64_t)(8 * q) * to.pitch) = *(const u32x4*)(lds + (8 * q + (lane >> 3)) * 64 + ((lane & 7) ^ (lane >> 3)) * 8);
+        };
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = 8 * g + 4 * h + e, turn = (4 * h + e) & 7;
+                lds[row * 64 + ((l32 >> 3) ^ turn) * 8 + (l32 & 7)] = hi[g][e];
+                lds[row * 64 + ((4 + (l32 >> 3)) ^ turn) * 8 + (l32 & 7)] = lo[g][e];
+            }
+        store(fin.C, r0, c0);
         // the same values the other way round; a diagonal tile has its own mirror image in it
         if (MODE == STEP || mirror) {
-            const Parts& t = MODE == STEP ? fin.Ct : fin.C;
-            f16* tp = t.p + b * t.batch + c * t.pitch + at_r;
-            *(f16x4*)tp = hi;
-            *(f16x4*)(tp + 32) = lo;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                *(f16x4*)(lds + l32 * 64 + (g ^ (l32 & 7)) * 8 + 4 * h) = hi[g];
+                *(f16x4*)(lds + l32 * 64 + ((4 + g) ^ (l32 & 7)) * 8 + 4 * h) = lo[g];
+            }
+            store(MODE == STEP ? fin.Ct : fin.C, c0, r0);
         }
     }
 }
@@ -230,23 +262,21 @@ __device__ __forceinline__ void tile_place(int at, int tiles_r, int tiles_c, int
 // C = A B^T of padded matrices in parts, both along the summed index: tiles of 32 WR RB x 32 WC CB, WR x WC waves with RB x CB
 // instruction tiles of 32 x 32 each. Blocks of 32 of the summed index go straight to LDS, NST - 1 on their way while one is multiplied; a row's
 // eight pieces of 16 bytes are stored in an order turned by the row's number, so that the reads of eight rows meet
-// different banks. (The loads deposit in lane order: it is their addresses that are turned.) KS > 1: as many such groups of waves take the
-// blocks of the summed index in turn, and the first adds up what they have: a tile alone on a CU waits for its own loads and LDS
-// reads most of the time. splits > 1: as many work-groups have a tile, each a part of the summed index, and leave their sums to
+// different banks. (The loads deposit in lane order: it is their addresses that are turned.) splits > 1: as
+// many work-groups have a tile, each a part of the summed index, and leave their sums to
 // ortho_join_kernel.
-template <int WR, int WC, int RB, int CB, int KS, int NST, int MODE>
-__global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin,
+template <int WR, int WC, int RB, int CB, int NST, int MODE>
+__global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin,
                                                                                int tile0, int splits, f32x4* __restrict__ partial) {
     constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, THREADS = WR * WC * 64;
     constexpr int STAGE = (TM + TN) * 8;  // pieces of 16 bytes
     constexpr int LOADS = STAGE / THREADS;
     static_assert(STAGE % THREADS == 0 && TM * 8 % THREADS == 0, "whole loads");
     static_assert(LOADS * (NST - 1) < 64, "a wait counts up to 63");
-    static_assert(KS == 1 || (KS - 1) * RB * CB * 4 * THREADS <= KS * NST * STAGE, "room for the sums");
-    extern __shared__ u32x4 lds[];  // KS * NST * STAGE
+    extern __shared__ u32x4 lds[];  // NST * STAGE
     constexpr bool SYM = MODE == GRAM || MODE == POLY;
     const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
-    constexpr bool SPLIT = RB == 2 && KS == 1;
+    constexpr bool SPLIT = RB == 2;
     const int unit = tile_in_turn(blockIdx.x, gridDim.x);
     const int tile = tile0 + (SPLIT ? unit / splits : unit), part = SPLIT ? unit % splits : 0;
     const int64_t b = tile / per;
@@ -255,12 +285,10 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
     if (SPLIT) kblocks = kblocks * (part + 1) / splits - first;
     int ti, tj;
     tile_place<SYM>(at, tiles_r, tiles_c, ti, tj);
-    const int group = KS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
-    const int tid = threadIdx.x - group * THREADS, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, h = lane >> 5;
     const int wr = wave / WC, wc = wave % WC;
-    u32x4* const ring = lds + group * NST * STAGE;
 
     // (a thread's pieces are in rows THREADS / 8 apart: one offset for each factor, the rest is the same for all threads)
     static_assert(THREADS % 64 == 0, "whole turns of 8 rows");
@@ -274,7 +302,7 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
             const int row = q * (THREADS / 8);
             const f16* from = row < TM ? abase + (int64_t)row * A.pitch + (int64_t)kb * 64 : bbase + (int64_t)(row - TM) * B.pitch + (int64_t)kb * 64;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (row < TM ? aoff : boff)),
-                                             (__attribute__((address_space(3))) void*)(ring + buf * STAGE + q * THREADS + wave * 64), 16, 0, 0);
+                                             (__attribute__((address_space(3))) void*)(lds + buf * STAGE + q * THREADS + wave * 64), 16, 0, 0);
         }
     };
 
@@ -292,7 +320,7 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
     };
     const int arow = wr * 32 * RB + l32, brow = TM + wc * 32 * CB + l32;
     auto read = [&](Factors& f, int buf, int s) __attribute__((always_inline)) {
-        const u32x4* st = ring + buf * STAGE;
+        const u32x4* st = lds + buf * STAGE;
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
             const int piece = (4 * p + 2 * s + h) ^ (l32 & 7);
@@ -316,7 +344,7 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
     // NST blocks are on their way before the first is used. (Beyond the end the last block is loaded again and not used, so that every turn
     // waits for the same number of loads.)
 #pragma unroll
-    for (int i = 0; i < NST; ++i) stage(min(i * KS + group, kblocks - 1), i);
+    for (int i = 0; i < NST; ++i) stage(min(i, kblocks - 1), i);
     auto meet = [&](auto wait) __attribute__((always_inline)) {  // the next block has landed; everyone has read the one before it
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(decltype(wait)::value);
@@ -328,46 +356,16 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
     meet(std::integral_constant<int, wait_for_loads(LOADS * (NST - 1))>{});
     read(f0, 0, 0);
     int buf = 0;
-    for (int kb = group; kb < kblocks + group; kb += KS) {
-        const bool some = KS == 1 || kb < kblocks;  // (the last turn has blocks for some groups only)
+    for (int kb = 0; kb < kblocks; ++kb) {
         read(f1, buf, 1);
-        if (some) multiply(f0);
+        multiply(f0);
         meet(std::integral_constant<int, wait_for_loads(LOADS * (NST - 2)) & ~0x0F00>{});  // (and nothing of this block is still being read from LDS)
-        stage(min(kb + NST * KS, kblocks - 1), buf);
+        stage(min(kb + NST, kblocks - 1), buf);
         buf = buf == NST - 1 ? 0 : buf + 1;
         read(f0, buf, 0);
-        if (some) multiply(f1);
+        multiply(f1);
     }
-    __builtin_amdgcn_s_waitcnt(wait_for_loads(0));  // nothing on its way to LDS when the work-group ends or uses it otherwise
-    if constexpr (KS > 1) {
-        f32x4* sums = (f32x4*)lds;
-        __syncthreads();
-        if (group > 0) {
-#pragma unroll
-            for (int i = 0; i < RB; ++i)
-#pragma unroll
-                for (int j = 0; j < CB; ++j)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g)
-                        sums[(((group - 1) * RB + i) * CB + j) * 4 * THREADS + g * THREADS + tid] =
-                            f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-        }
-        __syncthreads();
-        if (group > 0) return;
-#pragma unroll
-        for (int q = 0; q < KS - 1; ++q)
-#pragma unroll
-            for (int i = 0; i < RB; ++i)
-#pragma unroll
-                for (int j = 0; j < CB; ++j)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const f32x4 v = sums[((q * RB + i) * CB + j) * 4 * THREADS + g * THREADS + tid];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] += v[e];
-                    }
-    }
-
+    __builtin_amdgcn_s_waitcnt(wait_for_loads(0));  // nothing on its way to LDS when the work-group ends or uses LDS otherwise
     if (SPLIT && splits > 1) {
         // the sums of this part of the summed index, in the threads' own order
         f32x4* to = partial + ((int64_t)unit * RB * CB * 4) * THREADS + tid;
@@ -380,15 +378,17 @@ __global__ __launch_bounds__(KS * WR * WC * 64) void ortho_product_kernel(Parts 
                     to[((i * CB + j) * 4 + g) * THREADS] = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
         return;
     }
-    // A lane has four consecutive rows of one column: entries 4 g .. 4 g + 3 are rows 8 g + 4 h + 0 .. 3.
+    if constexpr (MODE != LAST) __syncthreads();  // the rings are free
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
-        for (int j = 0; j < CB; ++j)
+        for (int j = 0; j < CB; ++j) {
+            f32x4 v[4];
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                finish<MODE>(fin, b, (int64_t)ti * TM + (wr * RB + i) * 32 + 8 * g + 4 * h, (int64_t)tj * TN + (wc * CB + j) * 32 + l32, ti != tj,
-                             f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+            for (int g = 0; g < 4; ++g) v[g] = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+            finish<MODE>(fin, b, (int64_t)ti * TM + (wr * RB + i) * 32, (int64_t)tj * TN + (wc * CB + j) * 32, ti != tj, v,
+                         (f16*)lds + wave * 2048);
+        }
 }
 
 // The same for few tiles: 64 x 64, all of it by each of four waves, which take the blocks of the summed index in turn and add up what
@@ -488,31 +488,38 @@ __global__ __launch_bounds__(256) void ortho_wave_kernel(Parts A, Parts B, int k
                 sums[((wave * 4 + 2 * i + j) * 4 + g) * 64 + lane] = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
     __syncthreads();
     const int i = wave >> 1, j = wave & 1;
+    f32x4 v[4];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        f32x4 v = sums[(wave * 4 + g) * 64 + lane];
+        v[g] = sums[(wave * 4 + g) * 64 + lane];
 #pragma unroll
-        for (int q = 1; q < KS; ++q) v += sums[((q * 4 + wave) * 4 + g) * 64 + lane];
-        finish<MODE>(fin, b, (int64_t)ti * 64 + i * 32 + 8 * g + 4 * h, (int64_t)tj * 64 + j * 32 + l32, ti != tj, v);
+        for (int q = 1; q < KS; ++q) v[g] += sums[((q * 4 + wave) * 4 + g) * 64 + lane];
     }
+    finish<MODE>(fin, b, (int64_t)ti * 64 + i * 32, (int64_t)tj * 64 + j * 32, ti != tj, v, (f16*)(lds + 4096) + wave * 2048);
 }
 
-// The sums of the parts added up, in their order, and finished: a work-group has the 4 KB that 256 threads wrote together.
+// The sums of the parts added up, in their order, and finished: a wave has one of the RB x CB blocks of one of theirs.
 template <int WR, int WC, int RB, int CB, int MODE>
-__global__ __launch_bounds__(WR * WC * 64) void ortho_join_kernel(const f32x4* __restrict__ partial, int tile0, int splits, int tiles_r, int tiles_c, Finish fin) {
-    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, THREADS = WR * WC * 64, PIECES = RB * CB * 4;
+__global__ __launch_bounds__(64) void ortho_join_kernel(const f32x4* __restrict__ partial, int tile0, int splits, int tiles_r, int tiles_c, Finish fin) {
+    constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, WAVES = WR * WC, BLOCKS = RB * CB;
     constexpr bool SYM = MODE == GRAM || MODE == POLY;
+    __shared__ u32x4 turn[256];
     const int per = SYM ? tiles_r * (tiles_r + 1) / 2 : tiles_r * tiles_c;
-    const int piece = blockIdx.x % PIECES, mine = blockIdx.x / PIECES, tile = tile0 + mine, at = tile % per;
+    const int wave = blockIdx.x % WAVES, block = blockIdx.x / WAVES % BLOCKS, mine = blockIdx.x / WAVES / BLOCKS;
+    const int tile = tile0 + mine, at = tile % per;
     const int64_t b = tile / per;
     int ti, tj;
     tile_place<SYM>(at, tiles_r, tiles_c, ti, tj);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, h = lane >> 5;
-    const int wr = wave / WC, wc = wave % WC, i = piece / 4 / CB, j = piece / 4 % CB, g = piece % 4;
-    const f32x4* from = partial + ((int64_t)mine * splits * PIECES + piece) * THREADS + tid;
-    f32x4 v = from[0];
-    for (int q = 1; q < splits; ++q) v += from[(int64_t)q * PIECES * THREADS];
-    finish<MODE>(fin, b, (int64_t)ti * TM + (wr * RB + i) * 32 + 8 * g + 4 * h, (int64_t)tj * TN + (wc * CB + j) * 32 + l32, ti != tj, v);
+    const int wr = wave / WC, wc = wave % WC, i = block / CB, j = block % CB;
+    const f32x4* from = partial + ((int64_t)mine * splits * BLOCKS * 4 + block * 4) * (WAVES * 64) + wave * 64 + threadIdx.x;
+    f32x4 v[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) v[g] = from[g * (WAVES * 64)];
+#pragma unroll 4
+    for (int q = 1; q < splits; ++q)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) v[g] += from[((int64_t)q * BLOCKS * 4 + g) * (WAVES * 64)];
+    finish<MODE>(fin, b, (int64_t)ti * TM + (wr * RB + i) * 32, (int64_t)tj * TN + (wc * CB + j) * 32, ti != tj, v, (f16*)turn);
 }
 
 // ---- the plan ---------------------------------------------------------------------------------------------------
@@ -557,7 +564,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     const int side = p.huge ? 256 : p.big ? 128 : 64;
     p.M = padded(p.m, side);
     p.N = padded(p.n, side);
-    p.groups = (int)std::min<int64_t>(rows, std::max<int64_t>(1, std::min<int64_t>(256, rows * cols / 4096)));
+    p.groups = (int)std::min<int64_t>((rows + 3) / 4, std::max<int64_t>(1, std::min<int64_t>(256, rows * cols / 4096)));
     p.x = 2 * p.M * p.N;
     p.a = 2 * p.M * p.M;
     p.per = (3 * p.x + 2 * p.a) * 2 + align256(8 * p.groups);
@@ -602,7 +609,7 @@ hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols
                       f32x4* partial, hipStream_t st) {
     constexpr int WR = 2, CB = 2, THREADS = WR * WC * 64;
     constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, BYTES = NST * (TM + TN) * 128;
-    const auto kernel = ortho_product_kernel<WR, WC, RB, CB, 1, NST, MODE>;
+    const auto kernel = ortho_product_kernel<WR, WC, RB, CB, NST, MODE>;
     if (hipError_t e = ensure_dynamic_lds((const void*)kernel, BYTES); e != hipSuccess) return e;
     const int tr = (int)(rows / TM), tc = (int)(cols / TN), kb = (int)(k / KB);
     const int64_t tiles = tiles_of<MODE>(rows, cols, TM) * batch, rest = tiles % slots;
@@ -616,7 +623,7 @@ hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols
         if (splits > 1) {
             kernel<<<dim3((unsigned)(rest * splits)), THREADS, BYTES, st>>>(A, B, kb, tr, tc, fin, (int)whole, splits, partial);
             if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-            ortho_join_kernel<WR, WC, RB, CB, MODE><<<dim3((unsigned)(rest * RB * CB * 4)), THREADS, 0, st>>>(partial, (int)whole, splits, tr, tc, fin);
+            ortho_join_kernel<WR, WC, RB, CB, MODE><<<dim3((unsigned)(rest * RB * CB * WR * WC)), 64, 0, st>>>(partial, (int)whole, splits, tr, tc, fin);
         }
     }
     return hipGetLastError();
