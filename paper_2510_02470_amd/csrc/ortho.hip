@@ -44,6 +44,11 @@ __device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
     lo = (f16)(v - (float)hi);
 }
 
+__device__ __forceinline__ void split4(const f32x4& v, f16x4& hi, f16x4& lo) {
+    hi = __builtin_convertvector(v, f16x4);
+    lo = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
+}
+
 // ---- X: the norm, and the matrix in parts both ways -------------------------------------------------------------
 
 constexpr int NORM_THREADS = 256;
@@ -193,14 +198,7 @@ __device__ __forceinline__ void finish(const Finish& fin, int64_t b, int64_t r0,
         }
         f16x4 hi[4], lo[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                f16 x, y;
-                split(v[g][e], x, y);
-                hi[g][e] = x;
-                lo[g][e] = y;
-            }
+        for (int g = 0; g < 4; ++g) split4(v[g], hi[g], lo[g]);
         // 16 bytes of a line at a time; where they lie in LDS is turned by the row, so that rows meet different banks
         auto store = [&](const Parts& to, int64_t row, int64_t col) __attribute__((always_inline)) {
             f16* p = to.p + b * to.batch + (row + (lane >> 3)) * to.pitch + col * 2 + (lane & 7) * 8;
@@ -522,10 +520,254 @@ __global__ __launch_bounds__(64) void ortho_join_kernel(const f32x4* __restrict_
     finish<MODE>(fin, b, (int64_t)ti * TM + (wr * RB + i) * 32, (int64_t)tj * TN + (wc * CB + j) * 32, ti != tj, v, (f16*)turn);
 }
 
+// ---- small matrices ---------------------------------------------------------------------------------------------
+
+constexpr int SMALL_M = 64, SMALL_N = 512, MAX_STEPS = 32;
+
+// What the steps of a call need, for any matrix of it.
+struct Steps {
+    int count;
+    double eps, sx;  // X is kept as sx * X at first
+    struct {
+        float gram;        // X X^T as it is summed -> A, or straight to P where there is no A A
+        float square, linear, diag;  // A A, A and 1 -> P
+        float step;        // P X -> the next X, or the result
+        int cubic;
+    } at[MAX_STEPS];
+};
+
+// Up to 64 x 512 (m <= n), all steps by one work-group, which keeps X in registers: each wave has 64 columns of it, once with a lane for a
+// row (as X X^T takes it) and once with a lane for a column (as P X takes it). The instruction leaves a lane with four consecutive
+// entries along the other side, and two halves of a wave swap registers to make eight of them: P X is formed both ways, X P' and P X, in
+// place of a transposition through LDS. A is summed over the waves in LDS. WAVES: at most; four may have the registers of eight.
+template <class T, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int rows, int cols, int64_t ld, int64_t stride, T* out, int64_t ld_out,
+                                                          int64_t stride_out, Steps p) {
+    extern __shared__ u32x4 lds[];
+    __shared__ double norms[8];
+    const int W = blockDim.x >> 6, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, h = lane >> 5;
+    const bool tall = rows > cols;
+    const int m = tall ? cols : rows, n = tall ? rows : cols;
+    const int c0 = wave * 64;
+
+    // the wave's 64 x 64 entries, coalesced; scaled and split they go through LDS to the lanes that have them as factors
+    const T* g = G + (int64_t)blockIdx.x * stride;
+    float x[64];
+#pragma unroll
+    for (int i = 0; i < 64; ++i) {
+        const int r = tall ? lane : i, c = c0 + (tall ? i : lane);
+        x[i] = r < m && c < n ? RowType<T>::widen(tall ? g[(int64_t)c * ld + r] : g[(int64_t)r * ld + c]) : 0.f;
+    }
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) s = __builtin_fma((double)x[i], (double)x[i], s);
+    for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    if (lane == 0) norms[wave] = s;
+    __syncthreads();
+    s = norms[0];
+    for (int w = 1; w < W; ++w) s += norms[w];
+    // x * inv in fp32, of which inv may be out of range: a power of two first
+    const double inv = s > 0.0 || s != s ? p.sx / (sqrt(s) + p.eps) : 0.0;
+    const int power = ilogb(inv == 0.0 ? 1.0 : inv);
+    const float rest = (float)ldexp(inv, -power);
+    uint32_t* xs = (uint32_t*)lds + wave * (64 * 65);
+#pragma unroll
+    for (int i = 0; i < 64; ++i) {
+        f16 hi, lo;
+        split(ldexpf(x[i], power) * rest, hi, lo);
+        xs[(tall ? lane : i) * 65 + (tall ? i : lane)] = (uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
+    }
+    f16x8 by_row[2][4][2], by_col[2][4][2];  // [32 rows or columns][16 of the others][high, low]
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int way = 0; way < 2; ++way) {
+                u32x4 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t u[2];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int along = 16 * k + 8 * h + 2 * e + q, across = 32 * i + l32;
+                        u[q] = xs[way ? along * 65 + across : across * 65 + along];
+                    }
+                    hi[e] = (u[0] & 0xFFFFu) | u[1] << 16;
+                    lo[e] = u[0] >> 16 | (u[1] & 0xFFFF0000u);
+                }
+                (way ? by_col : by_row)[i][k][0] = __builtin_bit_cast(f16x8, hi);
+                (way ? by_col : by_row)[i][k][1] = __builtin_bit_cast(f16x8, lo);
+            }
+    __syncthreads();
+
+    f32x4* const sums = (f32x4*)lds;               // per wave three blocks of 32 x 32 of X X^T: (0, 0), (1, 0), (1, 1)
+    f16* const A = (f16*)(lds + W * 768);          // 64 rows of two blocks of 128 bytes, pieces turned by the row
+    f16* const P = A + 64 * 128;
+    auto at_part = [&](int r, int c) __attribute__((always_inline)) { return r * 128 + (c >> 5) * 64 + (((c & 31) >> 3 ^ (r & 7)) << 3) + (c & 7); };
+    // (the low part is four pieces further, before the turn: one bit of the piece's number)
+    auto put = [&](f16* to, int r, int c, const f32x4& v) __attribute__((always_inline)) {  // rows r .. r + 3 of column c, and the mirror image
+        f16x4 hi, lo;
+        split4(v, hi, lo);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            to[at_part(r + e, c)] = hi[e];
+            to[at_part(r + e, c) ^ 32] = lo[e];
+        }
+        if (r >> 5 != c >> 5) {
+            *(f16x4*)(to + at_part(c, r)) = hi;
+            *(f16x4*)(to + (at_part(c, r) ^ 32)) = lo;
+        }
+    };
+    auto part = [&](const f16* from, int block, int k, int which) __attribute__((always_inline)) {  // a lane's factor: row 32 block + l32, 16 k + 8 h ..
+        return *(const f16x8*)(from + (at_part(32 * block + l32, 16 * k + 8 * h) ^ which * 32));
+    };
+    auto product = [&](f32x16& acc, const f16x8* a, const f16x8* b) __attribute__((always_inline)) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1], b[0], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[1], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[0], acc, 0, 0, 0);
+    };
+    // entries v[4 g + e] (8 g + 4 h + e along one side, l32 along the other), scaled, as factors of the next products
+    auto refill = [&](f16x8 (*to)[2], const f32x16& v, float f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            f16x4 parts[2][2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                split4(f32x4{v[8 * k + 4 * q], v[8 * k + 4 * q + 1], v[8 * k + 4 * q + 2], v[8 * k + 4 * q + 3]} * f, parts[0][q], parts[1][q]);
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                const u32x2 x = __builtin_bit_cast(u32x2, parts[w][0]), y = __builtin_bit_cast(u32x2, parts[w][1]);
+                const auto u0 = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
+                const auto u1 = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
+                to[k][w] = __builtin_bit_cast(f16x8, u32x4{u0[0], u1[0], u0[1], u1[1]});
+            }
+        }
+    };
+    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+
+#pragma unroll 1
+    for (int step = 0; step < p.count; ++step) {
+        const auto q = p.at[step];
+        {
+            f32x16 acc[3] = {zero, zero, zero};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                product(acc[0], by_row[0][k], by_row[0][k]);
+                product(acc[1], by_row[1][k], by_row[0][k]);
+                product(acc[2], by_row[1][k], by_row[1][k]);
+            }
+#pragma unroll
+            for (int b = 0; b < 3; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    sums[wave * 768 + (b * 4 + j) * 64 + lane] = f32x4{acc[b][4 * j], acc[b][4 * j + 1], acc[b][4 * j + 2], acc[b][4 * j + 3]};
+        }
+        __syncthreads();
+        for (int i = wave; i < 12; i += W) {
+            const int b = i >> 2, j = i & 3, r = (b ? 32 : 0) + 8 * j + 4 * h, c = (b == 2 ? 32 : 0) + l32;
+            f32x4 v = sums[i * 64 + lane];
+            for (int w = 1; w < W; ++w) v += sums[w * 768 + i * 64 + lane];
+            v *= q.gram;
+            if (!q.cubic) {
+                put(A, r, c, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += r + e == c ? q.diag : 0.f;
+                put(P, r, c, v);
+            }
+        }
+        __syncthreads();
+        if (!q.cubic) {
+            for (int b = wave; b < 3; b += W) {
+                f32x16 acc = zero;
+                const int rb = b ? 1 : 0, cb = b == 2 ? 1 : 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const f16x8 x[2] = {part(A, rb, k, 0), part(A, rb, k, 1)}, y[2] = {part(A, cb, k, 0), part(A, cb, k, 1)};
+                    product(acc, x, y);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = 32 * rb + 8 * j + 4 * h, c = 32 * cb + l32;
+                    const f16x4 hi = *(const f16x4*)(A + at_part(c, r)), lo = *(const f16x4*)(A + (at_part(c, r) ^ 32));
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[e] = acc[4 * j + e] * q.square + ((float)hi[e] + (float)lo[e]) * q.linear + (r + e == c ? q.diag : 0.f);
+                    put(P, r, c, v);
+                }
+            }
+            __syncthreads();
+        }
+        const bool last = step + 1 == p.count;
+        T* const to = out + (int64_t)blockIdx.x * stride_out;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {  // 32 columns
+            f16x8 fresh[4][2];
+            if (!last || tall) {  // X' P: a lane has a row, four consecutive columns
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    asm volatile("" ::: "memory");  // (P's factors are read again rather than kept: registers)
+                    f32x16 acc = zero;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const f16x8 x[2] = {part(P, i, k, 0), part(P, i, k, 1)};
+                        product(acc, by_col[j][k], x);
+                    }
+                    if (!last) {
+                        refill(&by_row[i][2 * j], acc, q.step);
+                    } else {
+                        const int c = 32 * i + l32;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int r = c0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
+                            if (c < m && r < n) to[(int64_t)r * ld_out + c] = RowType<T>::narrow(acc[e] * q.step);
+                        }
+                    }
+                }
+            }
+            if (!last || !tall) {  // P X: a lane has a column, four consecutive rows
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    asm volatile("" ::: "memory");  // (P's factors are read again rather than kept: registers)
+                    f32x16 acc = zero;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const f16x8 x[2] = {part(P, i, k, 0), part(P, i, k, 1)};
+                        product(acc, x, by_col[j][k]);
+                    }
+                    if (!last) {
+                        refill(&fresh[2 * i], acc, q.step);
+                    } else {
+                        const int c = c0 + 32 * j + l32;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int r = 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
+                            if (r < m && c < n) to[(int64_t)r * ld_out + c] = RowType<T>::narrow(acc[e] * q.step);
+                        }
+                    }
+                }
+            }
+            if (!last) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) by_col[j][k][w] = fresh[k][w];
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (both at once would need more registers than there are)
+        }
+    }
+}
+
 // ---- the plan ---------------------------------------------------------------------------------------------------
 
-constexpr int MAX_SIDE = 32768, MAX_STEPS = 32;
-constexpr int64_t WORK_LIMIT = 1ll << 30;  // batches are taken in chunks that need no more, or one matrix at a time
+constexpr int MAX_SIDE = 32768;
+// batches are taken in chunks that need no more than 1 GB in all, or one matrix at a time
+constexpr int64_t WORK_LIMIT = (1ll << 30) - 512 * 128 * 128 * 4;
 
 template <int MODE>
 int64_t tiles_of(int64_t rows, int64_t cols, int64_t side) {
@@ -535,6 +777,7 @@ int64_t tiles_of(int64_t rows, int64_t cols, int64_t side) {
 
 struct Plan {
     int64_t m, n, M, N;  // the sides, smaller first, and padded
+    bool small;          // one work-group each, without work space
     bool huge;           // tiles of 256 x 256
     bool big;            // tiles of 128 x 128, else 64 x 64
     int groups;          // of rows, for the norm
@@ -558,6 +801,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     Plan p;
     p.m = std::min(rows, cols);
     p.n = std::max(rows, cols);
+    p.small = p.m <= SMALL_M && p.n <= SMALL_N;
     const int64_t tiles = (p.m + 127) / 128 * ((p.n + 127) / 128) * batch;
     p.big = p.m > 64 && tiles >= BIG_FROM;  // (a side of up to 64 would be padded to twice that and more)
     p.huge = p.m > 192 && (p.m + 255) / 256 * ((p.n + 255) / 256) * batch >= HUGE_FROM;
@@ -570,6 +814,10 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     p.per = (3 * p.x + 2 * p.a) * 2 + align256(8 * p.groups);
     p.chunk = std::max<int64_t>(1, std::min(batch, WORK_LIMIT / p.per));
     p.bytes = p.per * p.chunk + (p.big ? JOIN_BYTES : 0);
+    if (p.small) {
+        p.chunk = std::min<int64_t>(batch, 1 << 20);  // (a launch has fewer than 2^32 threads)
+        p.bytes = 256;  // (nothing of it is used)
+    }
     return p;
 }
 
@@ -645,6 +893,33 @@ template <class T>
 hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride, const float* coef, int steps,
                double eps, double scale, T* out, int64_t ld_out, int64_t stride_out, char* work, hipStream_t st) {
     const bool tall = rows > cols;
+    if (p.small) {
+        Steps q{};
+        q.count = steps;
+        q.eps = eps;
+        double U = 1.0 + 0x1p-10, sx = scale_for(U);
+        q.sx = sx;
+        for (int s = 0; s < steps; ++s) {
+            const double ca = coef[3 * s], cb = coef[3 * s + 1], cc = coef[3 * s + 2];
+            const double next = bound_of(ca, cb, cc, U, true) * (1.0 + 0x1p-10);
+            const double sa = scale_for(U * U), sp = scale_for(bound_of(ca, cb, cc, U * U, false)), sn = scale_for(next);
+            auto& a = q.at[s];
+            a.cubic = cc == 0.0;
+            a.gram = (float)(a.cubic ? cb * sp / (sx * sx) : sa / (sx * sx));
+            a.square = (float)(cc * sp / (sa * sa));
+            a.linear = (float)(cb * sp / sa);
+            a.diag = (float)(ca * sp);
+            a.step = (float)((s + 1 < steps ? sn : scale) / (sp * sx));
+            U = next;
+            sx = sn;
+        }
+        const int waves = (int)(p.n + 63) / 64;
+        const auto bytes = [](int w) { return std::max(w * 64 * 65 * 4, w * 12288 + 32768); };
+        const auto kernel = waves <= 4 ? ortho_small_kernel<T, 4> : ortho_small_kernel<T, 8>;
+        if (hipError_t e = ensure_dynamic_lds((const void*)kernel, bytes(waves <= 4 ? 4 : 8)); e != hipSuccess) return e;
+        kernel<<<dim3((unsigned)batch), waves * 64, bytes(waves), st>>>(G, (int)rows, (int)cols, ld, stride, out, ld_out, stride_out, q);
+        return hipGetLastError();
+    }
     f16* w = (f16*)work;
     const int64_t c = p.chunk;
     Parts X{w, 2 * p.N, p.x}, Xt[2] = {{w + c * p.x, 2 * p.M, p.x}, {w + 2 * c * p.x, 2 * p.M, p.x}};
