@@ -550,7 +550,8 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
     const int l32 = lane & 31, h = lane >> 5;
     const bool tall = rows > cols;
     const int m = tall ? cols : rows, n = tall ? rows : cols;
-    const int c0 = wave * 64;
+    const int c0 = wave * 64, used = (n + 63) >> 6;  // waves behind the last column only help with A and P
+    const bool mine = wave < used;
 
     // the wave's 64 x 64 entries, coalesced; scaled and split they go through LDS to the lanes that have them as factors
     const T* g = G + (int64_t)blockIdx.x * stride;
@@ -567,7 +568,7 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
     if (lane == 0) norms[wave] = s;
     __syncthreads();
     s = norms[0];
-    for (int w = 1; w < W; ++w) s += norms[w];
+    for (int w = 1; w < used; ++w) s += norms[w];
     // x * inv in fp32, of which inv may be out of range: a power of two first
     const double inv = s > 0.0 || s != s ? p.sx / (sqrt(s) + p.eps) : 0.0;
     const int power = ilogb(inv == 0.0 ? 1.0 : inv);
@@ -624,11 +625,10 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
     auto part = [&](const f16* from, int block, int k, int which) __attribute__((always_inline)) {  // a lane's factor: row 32 block + l32, 16 k + 8 h ..
         return *(const f16x8*)(from + (at_part(32 * block + l32, 16 * k + 8 * h) ^ which * 32));
     };
-    auto product = [&](f32x16& acc, const f16x8* a, const f16x8* b) __attribute__((always_inline)) {
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1], b[0], acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[1], acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[0], acc, 0, 0, 0);
-    };
+    // the three products of two parts each, several sums in turn: none waits for its own last
+    auto low_high = [&](f32x16& acc, const f16x8* a, const f16x8* b) __attribute__((always_inline)) { acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1], b[0], acc, 0, 0, 0); };
+    auto high_low = [&](f32x16& acc, const f16x8* a, const f16x8* b) __attribute__((always_inline)) { acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[1], acc, 0, 0, 0); };
+    auto high_high = [&](f32x16& acc, const f16x8* a, const f16x8* b) __attribute__((always_inline)) { acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[0], acc, 0, 0, 0); };
     // entries v[4 g + e] (8 g + 4 h + e along one side, l32 along the other), scaled, as factors of the next products
     auto refill = [&](f16x8 (*to)[2], const f32x16& v, float f) __attribute__((always_inline)) {
 #pragma unroll
@@ -652,13 +652,18 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
 #pragma unroll 1
     for (int step = 0; step < p.count; ++step) {
         const auto q = p.at[step];
-        {
+        if (mine) {
             f32x16 acc[3] = {zero, zero, zero};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                product(acc[0], by_row[0][k], by_row[0][k]);
-                product(acc[1], by_row[1][k], by_row[0][k]);
-                product(acc[2], by_row[1][k], by_row[1][k]);
+                const auto three = [&](auto one) __attribute__((always_inline)) {
+                    one(acc[0], by_row[0][k], by_row[0][k]);
+                    one(acc[1], by_row[1][k], by_row[0][k]);
+                    one(acc[2], by_row[1][k], by_row[1][k]);
+                };
+                three(low_high);
+                three(high_low);
+                three(high_high);
             }
 #pragma unroll
             for (int b = 0; b < 3; ++b)
@@ -670,7 +675,7 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
         for (int i = wave; i < 12; i += W) {
             const int b = i >> 2, j = i & 3, r = (b ? 32 : 0) + 8 * j + 4 * h, c = (b == 2 ? 32 : 0) + l32;
             f32x4 v = sums[i * 64 + lane];
-            for (int w = 1; w < W; ++w) v += sums[w * 768 + i * 64 + lane];
+            for (int w = 1; w < used; ++w) v += sums[w * 768 + i * 64 + lane];
             v *= q.gram;
             if (!q.cubic) {
                 put(A, r, c, v);
@@ -688,7 +693,9 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const f16x8 x[2] = {part(A, rb, k, 0), part(A, rb, k, 1)}, y[2] = {part(A, cb, k, 0), part(A, cb, k, 1)};
-                    product(acc, x, y);
+                    low_high(acc, x, y);
+                    high_low(acc, x, y);
+                    high_high(acc, x, y);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -705,60 +712,49 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
         }
         const bool last = step + 1 == p.count;
         T* const to = out + (int64_t)blockIdx.x * stride_out;
+        if (!mine) continue;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {  // 32 columns
-            f16x8 fresh[4][2];
-            if (!last || tall) {  // X' P: a lane has a row, four consecutive columns
+            f32x16 down[2] = {zero, zero}, along[2] = {zero, zero};  // P X: a lane has a column; X' P: a lane has a row
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    asm volatile("" ::: "memory");  // (P's factors are read again rather than kept: registers)
-                    f32x16 acc = zero;
+            for (int k = 0; k < 4; ++k) {
+                f16x8 x[2][2];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const f16x8 x[2] = {part(P, i, k, 0), part(P, i, k, 1)};
-                        product(acc, by_col[j][k], x);
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) x[i][w] = part(P, i, k, w);
+                const auto four = [&](auto one, auto other) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        one(down[i], x[i], by_col[j][k]);
+                        other(along[i], by_col[j][k], x[i]);
                     }
-                    if (!last) {
-                        refill(&by_row[i][2 * j], acc, q.step);
-                    } else {
-                        const int c = 32 * i + l32;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int r = c0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
-                            if (c < m && r < n) to[(int64_t)r * ld_out + c] = RowType<T>::narrow(acc[e] * q.step);
-                        }
-                    }
-                }
-            }
-            if (!last || !tall) {  // P X: a lane has a column, four consecutive rows
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    asm volatile("" ::: "memory");  // (P's factors are read again rather than kept: registers)
-                    f32x16 acc = zero;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const f16x8 x[2] = {part(P, i, k, 0), part(P, i, k, 1)};
-                        product(acc, x, by_col[j][k]);
-                    }
-                    if (!last) {
-                        refill(&fresh[2 * i], acc, q.step);
-                    } else {
-                        const int c = c0 + 32 * j + l32;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int r = 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
-                            if (r < m && c < n) to[(int64_t)r * ld_out + c] = RowType<T>::narrow(acc[e] * q.step);
-                        }
-                    }
-                }
+                };
+                four(low_high, high_low);
+                four(high_low, low_high);
+                four(high_high, high_high);
             }
             if (!last) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+                for (int i = 0; i < 2; ++i) {
+                    refill(&by_row[i][2 * j], along[i], q.step);
+                    refill(&by_col[j][2 * i], down[i], q.step);
+                }
+            } else {
+                // (the form in which a row of the result goes to consecutive lanes)
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) by_col[j][k][w] = fresh[k][w];
+                for (int i = 0; i < 2; ++i) {
+                    const int c = tall ? 32 * i + l32 : c0 + 32 * j + l32;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int r = (tall ? c0 + 32 * j : 32 * i) + 8 * (e >> 2) + 4 * h + (e & 3);
+                        if (r < rows && c < cols) to[(int64_t)r * ld_out + c] = RowType<T>::narrow((tall ? along[i][e] : down[i][e]) * q.step);
+                    }
+                }
             }
-            __builtin_amdgcn_sched_barrier(0);  // (both at once would need more registers than there are)
+            // (both at once would need more registers than there are, and P's factors are read again rather than kept)
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" ::: "memory");
         }
     }
 }
@@ -913,7 +909,8 @@ hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t c
             U = next;
             sx = sn;
         }
-        const int waves = (int)(p.n + 63) / 64;
+        // (a few matrices have four waves each for what is not split over columns)
+        const int waves = std::max((int)(p.n + 63) / 64, batch <= 512 ? 4 : 1);
         const auto bytes = [](int w) { return std::max(w * 64 * 65 * 4, w * 12288 + 32768); };
         const auto kernel = waves <= 4 ? ortho_small_kernel<T, 4> : ortho_small_kernel<T, 8>;
         if (hipError_t e = ensure_dynamic_lds((const void*)kernel, bytes(waves <= 4 ? 4 : 8)); e != hipSuccess) return e;
