@@ -65,13 +65,15 @@ __device__ __forceinline__ Cut cut_after(uint64_t listed) {  // the last that is
     return Cut{value_of((uint32_t)(listed >> 32)), (int)~(uint32_t)listed + 1};
 }
 
+constexpr int U = 2;  // vectors of a thread that are read together
+
 // What the THREADS threads of a row share.
 template <int THREADS>
 struct Shared {
     static constexpr int W = THREADS / 64;
     static constexpr int BITS = THREADS == 64 ? 8 : THREADS == 256 ? 10 : 11, BINS = 1 << BITS;  // of a histogram
     static constexpr int LIST = THREADS == 64 ? 128 : THREADS == 256 ? 512 : 1024;  // classes that are put in order one by one
-    static constexpr int SEGS = THREADS >= 512 ? SAGE_MAX_CLASSES / 1024 : W;  // pieces of 64 * U vectors of the longest row
+    static constexpr int SEGS = THREADS >= 512 ? SAGE_MAX_CLASSES / (256 * U) : 16 * W;  // pieces of 64 * U vectors of the longest row
     uint64_t hist[BINS];  // a histogram (of counts, weights, or approximate weights)
     uint64_t seg[SEGS];   // sums of segments
     uint64_t part[W];
@@ -85,7 +87,6 @@ struct Shared {
 
 __device__ __forceinline__ uint64_t mask_of(bool b) { return b ? ~0ull : 0ull; }
 
-constexpr int U = 4;  // vectors of a thread that are read together
 
 // A row as THREADS threads see it. A segment is 64 * U vectors, of which lane l of a wave has vectors l, 64 + l, ..; waves take
 // segments in turn. Elements behind the row's end are -inf. STAGED: the first pass leaves the row in LDS, else it is read again by
@@ -486,7 +487,7 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
 }
 
 template <class T, int THREADS, bool STAGED>
-__global__ __launch_bounds__(THREADS, THREADS == 512 ? 2 : 1) void sample_kernel(const T* __restrict__ logits, int C, int64_t ld, const float* __restrict__ u_rows,
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel(const T* __restrict__ logits, int C, int64_t ld, const float* __restrict__ u_rows,
                                                          sage_sampling how, int* __restrict__ labels, float* __restrict__ logp) {
     __shared__ Shared<THREADS> S;
     constexpr int VL = RowType<T>::VL, W = THREADS / 64, LIST = Shared<THREADS>::LIST;
