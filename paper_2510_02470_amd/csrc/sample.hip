@@ -445,6 +445,7 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
     for (int i = tid; i < count; i += THREADS) {
         const uint64_t key = S.lkey[i];
         int rank = 0;
+#pragma unroll 8
         for (int k = 0; k < count; ++k) rank += S.lkey[k] > key;
         S.sorted[rank] = key;
         S.sw[rank] = S.lw[i];
@@ -479,6 +480,7 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
     for (int i = tid; i < count; i += THREADS) {
         const uint64_t place = S.lkey[i];
         uint64_t before = 0;
+#pragma unroll 8
         for (int k = 0; k < count; ++k) before += S.lkey[k] < place ? S.lw[k] : 0;
         if (before <= t && before + S.lw[i] > t) S.answer = place;
     }
@@ -536,38 +538,49 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
     Cut cut{-INFINITY, 0};  // (-inf has no weight)
     if (K > 0 && K < C) {
         // the bin that the K-th is in; if all up to it can be listed, the rest is done on the list
-        const Bins bins(m, fminf(spread, 64.f), S.BINS);
+        const Bins kbins(m, fminf(spread, 64.f), S.BINS);
         uint32_t* counts = (uint32_t*)S.hist;
         clear_histogram(S, r.tid);
-        r.each([&](float x, int e) __attribute__((always_inline)) {
-            if (e < C) atomicAdd(&counts[bins(x)], 1u);
+        r.each([&](float x, int) __attribute__((always_inline)) {
+            if (x > -INFINITY) atomicAdd(&counts[kbins(x)], 1u);  // (masked classes, all in one bin, would wait for each other)
         });
         __syncthreads();
         uint64_t all;
         const int b = find_sum<THREADS>(S, counts, S.BINS, r.tid, all, [&](uint64_t) { return (uint64_t)K - 1; });
         const uint64_t through = S.found[0] + S.found[1];
-        if (through <= LIST) {
-            const float least = least_of_bin(bins, b);
-            const int count = collect(r, S, [&](float x, int e) __attribute__((always_inline)) { return (x >= least) & (e < C); },
+        if (all <= (uint64_t)K) {
+            // every class that has a weight is among the first K
+        } else if (through <= LIST) {
+            const float least = least_of_bin(kbins, b);
+            const int count = collect(r, S, [&](float x, int) __attribute__((always_inline)) { return (x >= least) & (x > -INFINITY); },
                                       [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) | 1ull << 63; });
             for (int i = r.tid; i < count; i += THREADS) S.lw[i] &= ~(1ull << 63);  // (without a weight they count for top-k all the same)
             __syncthreads();
             j = draw_listed(r, S, count, K, P32, border, md, u, total);
         } else {
-            cut = front(r, S, (uint64_t)K - 1, bins, [&](float, int e) __attribute__((always_inline)) { return e < C ? 1ull : 0ull; });
+            cut = front(r, S, (uint64_t)K - 1, kbins, [&](float x, int) __attribute__((always_inline)) { return x > -INFINITY ? 1ull : 0ull; });
         }
     }
-    if (j < 0 && P32 < 1.f) {
+    const Bins bins(m, fminf(spread, 30.f * T32), S.BINS);
+    const bool cut_before = cut.place > 0;  // a top-k of more than the list holds: any row, any order of the cuts
+    if (cut_before && P32 < 1.f) {
+        uint64_t sum = 0;
+        r.each([&](float x, int e) __attribute__((always_inline)) { sum += weight(x, e) & mask_of(cut.keeps(x, e)); });
+        sum = group_sum<THREADS>(sum, S);
+        const double q = ceil((double)P32 * (double)sum);
+        const Cut k_cut = cut;
+        cut = front(r, S, q >= 1.0 ? (uint64_t)q - 1 : 0, bins,
+                    [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) & mask_of(k_cut.keeps(x, e)); });
+    }
+    if (j < 0 && P32 < 1.f && !cut_before) {
         // An approximate histogram says in which bin the border is likely to be. One exact pass then has the sum of all, for each segment the
         // sum of what is in the bins before, and a list of the bin itself, whose kept members are added to the segments one by one.
-        const Bins bins(m, fminf(spread, 30.f * T32), S.BINS);
-        auto in_cut = [&](float x, int e) __attribute__((always_inline)) { return cut.keeps(x, e); };
         const float c2 = (float)(inv * 1.4426950408889634);
         clear_histogram(S, r.tid);
-        r.each([&](float x, int e) __attribute__((always_inline)) {
+        r.each([&](float x, int) __attribute__((always_inline)) {
             // (whole numbers: adding floats in LDS takes ten times as long)
             const uint32_t w = (uint32_t)(__builtin_amdgcn_exp2f((x - m) * c2) * 0x1p31f);
-            if (in_cut(x, e)) atomicAdd((unsigned long long*)&S.hist[bins(x)], (unsigned long long)w);
+            if (w) atomicAdd((unsigned long long*)&S.hist[bins(x)], (unsigned long long)w);
         });
         __syncthreads();
         const int b = find_sum<THREADS>(S, S.hist, S.BINS, r.tid, total, [&](uint64_t all) { return share_of(P32, all); });
@@ -585,7 +598,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
                     if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
                     const float x = RowType<T>::at(v[q], k);
                     const int e = r.place(i, q) + k;
-                    const uint64_t w = (bits(x) - ROUND_BITS) & mask_of(in_cut(x, e));
+                    const uint64_t w = bits(x) - ROUND_BITS;
                     sum += w;
                     own += w & mask_of(x >= from);
                     if ((x < from) & (x >= least) & (w != 0)) {
@@ -615,6 +628,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
             for (int i = r.tid; i < listed; i += THREADS) {
                 const uint64_t key = S.lkey[i];
                 uint64_t ahead = before;
+#pragma unroll 8
                 for (int k = 0; k < listed; ++k) ahead += S.lkey[k] > key ? S.lw[k] : 0;
                 if (ahead < need) {
                     atomicAdd((unsigned long long*)&S.seg[r.segment_of((int)~(uint32_t)key)], (unsigned long long)S.lw[i]);
@@ -625,9 +639,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
             cut = cut_after(S.answer);
             __syncthreads();
             if ((double)cut.value - md >= border)  // (else min-p keeps less)
-                j = locate_in(r, S, total, &u, 0, [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) & mask_of(in_cut(x, e)); });
+                j = locate_in(r, S, total, &u, 0, [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) & mask_of(cut.keeps(x, e)); });
         } else {
-            cut = front(r, S, need - 1, bins, [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) & mask_of(in_cut(x, e)); });
+            cut = front(r, S, need - 1, bins, weight);
         }
     }
     if (j < 0)
@@ -662,6 +676,7 @@ hipError_t launch_sample(const void* logits, int64_t rows, int C, int64_t ld, co
         if (C <= 64 * 4 * VL) e = go(integral_constant<int, 64>{}, std::true_type{});
         else if (C <= 256 * 4 * VL) e = go(integral_constant<int, 256>{}, std::true_type{});
         else if (C <= 1024 * 4 * VL) e = go(integral_constant<int, 1024>{}, std::true_type{});
+        else if (rows <= 256) e = go(integral_constant<int, 1024>{}, std::false_type{});  // a CU has one of them, if any
         else e = go(integral_constant<int, 512>{}, std::false_type{});
         if (e != hipSuccess) return e;
         if (h.temperature_rows) h.temperature_rows += grid.x;
