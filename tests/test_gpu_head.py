@@ -112,6 +112,20 @@ def test_sample_draws_every_kept_class_as_often_as_it_should(how):
     assert np.abs(np.array([(labels == j).mean() for j in kept]) - share).max() <= 1 / 4096
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,C", [(3, 900), (3, 5000), (3, 40_000), (300, 20_000)])
+def test_sample_borders_among_many_classes(n, C, dtype):
+    """Top-k of more classes than are ranked one by one, borders of top-p in flat rows (a bin holds thousands), few distinct values."""
+    rng = np.random.default_rng(n + C)
+    z = 0.01 * rng.standard_normal((n, C))
+    z[1] = rng.integers(0, 3, C)
+    z[2] = 30 * rng.standard_normal(C)
+    u = rng.random(n, dtype=np.float32)
+    for how in (dict(top_k=C // 2), dict(top_k=C - 1, top_p=0.9), dict(top_p=0.7), dict(top_p=0.7, min_p=0.999), dict(top_k=C // 3, top_p=0.5, min_p=0.2),
+                dict(temperature=0.02, top_p=0.8)):
+        _check_sample(z, u, dtype, **how)
+
+
 def test_sample_random_numbers_at_and_beyond_the_ends():
     z, _ = _some_rows(8, 500, 3)
     z[:, 490:] = -np.inf  # the last class with a weight is not the last class
@@ -407,6 +421,42 @@ def test_orthogonalize_unusual_matrices(m, n, dtype):
     got = _check_ortho(stack, dtype, eps=0.0)
     assert not got[0].any()
     _check_ortho(stack, dtype, eps=1e-7)
+
+
+@pytest.mark.parametrize("b,m,n,dtype", [
+    (1, 1800, 1930, "f32"),      # tiles of 128 x 128, the left-over ones in parts
+    (1, 1930, 1800, "bf16"),
+    (1, 4000, 3600, "f32"),      # tiles of 256 x 256 for one of the products
+    (1, 512, 16_400, "bf16"),
+    (3, 700, 1300, "f32"),
+    (30, 513, 500, "bf16"),      # a batch of them
+    (60, 200, 300, "f32"),
+    (20, 65, 129, "f32"),        # just beyond the smallest ones
+    (700, 64, 512, "bf16"),      # the largest of the smallest ones, and more of them than have helping waves
+    (600, 64, 512, "f32"),
+])
+def test_orthogonalize_large(b, m, n, dtype):
+    """Against 64-bit products on the GPU (numpy would take minutes)."""
+    import torch
+    from paper_2510_02470_amd.binding import orthogonalize
+
+    g = torch.Generator(device="cuda").manual_seed(b + m + n)
+    G = (torch.randn(b, m, n, generator=g, device="cuda") * torch.rand(n, generator=g, device="cuda")).to(_tdtype(dtype))
+    out = orthogonalize(G, scale=0.5)
+    again = orthogonalize(G, scale=0.5)
+    assert torch.equal(out, again)
+    for i in sorted({0, b // 2, b - 1}):
+        X = G[i].double() if m <= n else G[i].double().T.contiguous()
+        X = X / (torch.linalg.vector_norm(X) + _f32(1e-7))
+        norms = []
+        for _ in range(5):
+            norms.append(float(torch.linalg.vector_norm(X)))
+            A = X @ X.T.contiguous()
+            X = _f32(MUON[0]) * X + (_f32(MUON[1]) * A + _f32(MUON[2]) * (A @ A)) @ X
+        want = 0.5 * (X if m <= n else X.T)
+        tol = ref.orthogonalize_bound(norms, [MUON] * 5, 0.5, m * n) + 1.01 * ref.HALF_STEP[dtype] * float(torch.linalg.vector_norm(want))
+        err = float(torch.linalg.vector_norm(out[i].double() - want))
+        assert err <= tol, (i, err, tol)
 
 
 def test_orthogonalize_gives_singular_values_near_one():
