@@ -78,10 +78,10 @@ struct Shared {
     uint64_t seg[SEGS];   // sums of segments
     uint64_t part[W];
     float fpart[2 * W];
-    uint64_t lkey[LIST], sorted[LIST];  // of listed classes key and place, one number in their common order
-    uint64_t lw[LIST], sw[LIST];        // and weight
+    uint64_t lkey[LIST], skey[LIST];  // of listed classes key and place, one number in their common order
+    uint64_t lw[LIST], sw[LIST];      // and weight
     uint64_t found[2];
-    unsigned listed;
+    unsigned listed, few;
     uint64_t answer;
 };
 
@@ -435,57 +435,71 @@ __device__ __forceinline__ Cut front(const Row<T, THREADS, STAGED>& r, Shared<TH
     }
 }
 
-// The listed classes (the first K of the order and maybe more) reduced by top-k, top-p and min-p, and the draw. They are ranked in the
-// order, and what is kept by place. K <= count <= LIST.
+// Of the members of the list (member(i)), in falling order of key(i), the one up to which f(i) sum to more than t, `above` being the sum
+// before the first of them: its key. They are few as a rule (of one bin, or of one segment): each looks at all others.
+template <int THREADS, class M, class K, class F>
+__device__ __forceinline__ uint64_t passing(Shared<THREADS>& S, int count, int tid, uint64_t above, uint64_t t, M member, K key, F f) {
+    __syncthreads();
+    if (tid == 0) S.few = 0;
+    __syncthreads();
+    for (int i = tid; i < count; i += THREADS)
+        if (member(i)) {
+            const unsigned p = atomicAdd(&S.few, 1u);
+            S.skey[p] = key(i);
+            S.sw[p] = f(i);
+        }
+    __syncthreads();
+    const int few = (int)S.few;
+    for (int i = tid; i < few; i += THREADS) {
+        const uint64_t mine = S.skey[i];
+        uint64_t before = above;
+#pragma unroll 8
+        for (int k = 0; k < few; ++k) before += S.skey[k] > mine ? S.sw[k] : 0;
+        if (before <= t && before + S.sw[i] > t) S.answer = mine;
+    }
+    __syncthreads();
+    return S.answer;
+}
+
+// The listed classes (those of bins up to b, in which the K-th of the order is, `before` of them in the bins before it) reduced by top-k,
+// top-p and min-p, and the draw.
 template <class T, int THREADS, bool STAGED>
-__device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, int count, int K, float P, double border,
-                           double md, float u, uint64_t& total) {
+__device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, int count, int K, const Bins& bins, int b,
+                                           uint64_t before, float P, double border, double md, float u, uint64_t& total) {
     const int tid = r.tid;
-    constexpr int PER = Shared<THREADS>::LIST / THREADS;  // listed classes of a thread
-    for (int i = tid; i < count; i += THREADS) {
-        const uint64_t key = S.lkey[i];
-        int rank = 0;
-#pragma unroll 8
-        for (int k = 0; k < count; ++k) rank += S.lkey[k] > key;
-        S.sorted[rank] = key;
-        S.sw[rank] = S.lw[i];
-    }
-    __syncthreads();
-    count = K;
-    // thread tid has ranks tid * PER ..
-    uint64_t own = 0;
-    for (int i = 0; i < PER; ++i)
-        if (tid * PER + i < count) own += S.sw[tid * PER + i];
+    auto value = [&](int i) __attribute__((always_inline)) { return value_of((uint32_t)(S.lkey[i] >> 32)); };
+    auto key = [&](int i) __attribute__((always_inline)) { return S.lkey[i]; };
+    auto weight = [&](int i) __attribute__((always_inline)) { return S.lw[i]; };
+    uint64_t last = passing(S, count, tid, before, (uint64_t)K - 1, [&](int i) __attribute__((always_inline)) { return bins(value(i)) == b; }, key,
+                            [](int) { return 1ull; });
     if (P < 1.f) {
-        const uint64_t sum = group_sum<THREADS>(own, S);
-        const double q = ceil((double)P * (double)sum);
-        const uint64_t need = q >= 1.0 ? (uint64_t)q : 1;
-        uint64_t all;
-        const int last = find_sum<THREADS>(S, S.sw, count, tid, all, [&](uint64_t) { return need - 1; });
-        count = last + 1;
+        clear_histogram(S, tid);
+        for (int i = tid; i < count; i += THREADS)
+            if (S.lkey[i] >= last) atomicAdd((unsigned long long*)&S.hist[bins(value(i))], (unsigned long long)S.lw[i]);
         __syncthreads();
+        uint64_t t = 0;
+        const int at = find_sum<THREADS>(S, S.hist, S.BINS, tid, total, [&](uint64_t all) {
+            const double q = ceil((double)P * (double)all);
+            return t = q >= 1.0 ? (uint64_t)q - 1 : 0;
+        });
+        const uint64_t above = S.found[0], top_k = last;
+        last = passing(S, count, tid, above, t,
+                       [&](int i) __attribute__((always_inline)) { return (S.lkey[i] >= top_k) & (bins(value(i)) == at); }, key, weight);
     }
-    // by place: the kept ones before each, and their weights
-    for (int i = tid; i < count; i += THREADS) {
-        const uint64_t key = S.sorted[i];
-        const bool kept = (double)value_of((uint32_t)(key >> 32)) - md >= border;
-        S.lkey[i] = kept ? (uint32_t)~(uint32_t)key : 0xFFFFFFFFu;
-        S.lw[i] = kept ? S.sw[i] : 0;
-    }
+    // the draw: the segments' sums, and the classes of one segment by their places
+    auto kept = [&](int i) __attribute__((always_inline)) { return (S.lkey[i] >= last) & ((double)value(i) - md >= border); };
+    auto place = [&](int i) __attribute__((always_inline)) { return (int)~(uint32_t)S.lkey[i]; };
     __syncthreads();
-    own = 0;
-    for (int i = tid; i < count; i += THREADS) own += S.lw[i];
-    total = group_sum<THREADS>(own, S);
-    const uint64_t t = share_of(u, total);
-    for (int i = tid; i < count; i += THREADS) {
-        const uint64_t place = S.lkey[i];
-        uint64_t before = 0;
-#pragma unroll 8
-        for (int k = 0; k < count; ++k) before += S.lkey[k] < place ? S.lw[k] : 0;
-        if (before <= t && before + S.lw[i] > t) S.answer = place;
-    }
+    for (int i = tid; i < r.count * r.W; i += THREADS) S.seg[i] = 0;
     __syncthreads();
-    return (int)S.answer;
+    for (int i = tid; i < count; i += THREADS)
+        if (kept(i)) atomicAdd((unsigned long long*)&S.seg[r.segment_of(place(i))], (unsigned long long)S.lw[i]);
+    __syncthreads();
+    const int seg = find_sum<THREADS>(S, S.seg, r.count * r.W, tid, total, [&](uint64_t all) { return share_of(u, all); });
+    const uint64_t base = S.found[0];
+    return (int)~(uint32_t)passing(S, count, tid, base, share_of(u, total),
+                                   [&](int i) __attribute__((always_inline)) { return kept(i) & (r.segment_of(place(i)) == seg); },
+                                   [&](int i) __attribute__((always_inline)) { return (uint64_t)(uint32_t)S.lkey[i]; }, weight);
 }
 
 template <class T, int THREADS, bool STAGED>
@@ -547,7 +561,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
         __syncthreads();
         uint64_t all;
         const int b = find_sum<THREADS>(S, counts, S.BINS, r.tid, all, [&](uint64_t) { return (uint64_t)K - 1; });
-        const uint64_t through = S.found[0] + S.found[1];
+        const uint64_t before = S.found[0], through = before + S.found[1];
         if (all <= (uint64_t)K) {
             // every class that has a weight is among the first K
         } else if (through <= LIST) {
@@ -556,7 +570,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
                                       [&](float x, int e) __attribute__((always_inline)) { return weight(x, e) | 1ull << 63; });
             for (int i = r.tid; i < count; i += THREADS) S.lw[i] &= ~(1ull << 63);  // (without a weight they count for top-k all the same)
             __syncthreads();
-            j = draw_listed(r, S, count, K, P32, border, md, u, total);
+            j = draw_listed(r, S, count, K, kbins, b, before, P32, border, md, u, total);
         } else {
             cut = front(r, S, (uint64_t)K - 1, kbins, [&](float x, int) __attribute__((always_inline)) { return x > -INFINITY ? 1ull : 0ull; });
         }
