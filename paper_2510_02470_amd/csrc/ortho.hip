@@ -787,7 +787,7 @@ int64_t padded(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
 // tiles of 128 x 128 of X, from which on they are used
-constexpr int64_t BIG_FROM = 200;
+constexpr int64_t BIG_FROM = 100;
 constexpr int64_t HUGE_FROM = 224;    // ... of 256 x 256
 constexpr int64_t SLOTS = 512;        // work-groups of 128 x 128 at a time, two to a CU
 constexpr int SPLIT_BLOCKS = 8;       // blocks of the summed index in a part of it, at least
@@ -846,10 +846,36 @@ double scale_for(double top) {
     return ldexp(1.0, 15 - e);
 }
 
-// `slots` work-groups run at a time. Tiles that are left over when the slots have been filled as often as possible are cut along the summed
-// index, so that they fill them too: 528 tiles of 128 x 128 of a 4096 x 4096 product take 275 us as they are and 215 so (512 whole ones and 16 in 32 parts).
+// How a product is cut. Estimates in microseconds, from products of 128 x 1024 (48 of them) to 4096 x 4096: a work-group of
+// ortho_wave_kernel, one to a CU, takes 1.0 for four blocks of the summed index and 3 for the rest of a tile of 64 x 64; a tile of
+// 128 x 128 takes 1.0 a block when it has a CU to itself, two on one take 1.6, and 4 for the rest. Tiles that are left over when the slots
+// have been filled as often as possible may be cut along the summed index, so that they fill them too: joining them takes a launch of
+// 6 and 0.03 a part (64 KB written and read). 528 tiles of a 4096 x 4096 product: 275 us as they are, 215 so (512 whole ones
+// and 16 in 32 parts); 48 products X X' of 128 x 1024: 18 in tiles of 128, 11 in tiles of 64.
+struct Cut {
+    bool waves;  // ortho_wave_kernel
+    int splits;  // of the tiles that are left over
+};
+
+Cut cut_of(int64_t tiles64, int64_t tiles128, int64_t blocks) {
+    const double waves = (double)((tiles64 + 255) / 256) * ((double)((blocks + 3) / 4) + 3.0);
+    const int64_t rest = tiles128 % SLOTS;
+    const double whole = (double)(tiles128 / SLOTS) * (1.6 * (double)blocks + 4.0);
+    Cut best{true, 1};
+    double least = waves;
+    for (int64_t s = 1; s <= (rest ? std::max<int64_t>(1, std::min<int64_t>(SLOTS / rest, blocks / SPLIT_BLOCKS)) : 1); ++s) {
+        double t = whole;
+        if (rest) t += (rest * s <= SLOTS / 2 ? 1.0 : 1.6) * (double)((blocks + s - 1) / s) + 4.0 + (s > 1 ? 6.0 + 0.03 * (double)(rest * s) : 0.0);
+        if (t < least) {
+            least = t;
+            best = Cut{false, (int)s};
+        }
+    }
+    return best;
+}
+
 template <int MODE, int WC, int RB, int NST>
-hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, int64_t slots,
+hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin, int64_t slots, int splits,
                       f32x4* partial, hipStream_t st) {
     constexpr int WR = 2, CB = 2, THREADS = WR * WC * 64;
     constexpr int TM = 32 * WR * RB, TN = 32 * WC * CB, BYTES = NST * (TM + TN) * 128;
@@ -857,7 +883,6 @@ hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols
     if (hipError_t e = ensure_dynamic_lds((const void*)kernel, BYTES); e != hipSuccess) return e;
     const int tr = (int)(rows / TM), tc = (int)(cols / TN), kb = (int)(k / KB);
     const int64_t tiles = tiles_of<MODE>(rows, cols, TM) * batch, rest = tiles % slots;
-    const int splits = RB == 2 && rest ? (int)std::max<int64_t>(1, std::min<int64_t>(slots / rest, kb / SPLIT_BLOCKS)) : 1;
     const int64_t whole = splits > 1 ? tiles - rest : tiles;
     if (whole) {
         kernel<<<dim3((unsigned)whole), THREADS, BYTES, st>>>(A, B, kb, tr, tc, fin, 0, 1, nullptr);
@@ -867,7 +892,8 @@ hipError_t product_of(const Parts& A, const Parts& B, int64_t rows, int64_t cols
         if (splits > 1) {
             kernel<<<dim3((unsigned)(rest * splits)), THREADS, BYTES, st>>>(A, B, kb, tr, tc, fin, (int)whole, splits, partial);
             if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-            ortho_join_kernel<WR, WC, RB, CB, MODE><<<dim3((unsigned)(rest * RB * CB * WR * WC)), 64, 0, st>>>(partial, (int)whole, splits, tr, tc, fin);
+            ortho_join_kernel<WR, WC, RB, CB, MODE>
+                <<<dim3((unsigned)(rest * RB * CB * WR * WC)), 64, 0, st>>>(partial, (int)whole, splits, tr, tc, fin);
         }
     }
     return hipGetLastError();
@@ -877,8 +903,11 @@ template <int MODE>
 hipError_t product(const Plan& p, const Parts& A, const Parts& B, int64_t rows, int64_t cols, int64_t k, int64_t batch, const Finish& fin,
                    f32x4* partial, hipStream_t st) {
     // (half of a square is too few tiles of 256 x 256)
-    if (p.huge && (MODE == STEP || MODE == LAST)) return product_of<MODE, 4, 4, 2>(A, B, rows, cols, k, batch, fin, 256, nullptr, st);
-    if (p.big) return product_of<MODE, 2, 2, 2>(A, B, rows, cols, k, batch, fin, SLOTS, partial, st);
+    if (p.huge && (MODE == STEP || MODE == LAST)) return product_of<MODE, 4, 4, 2>(A, B, rows, cols, k, batch, fin, 256, 1, nullptr, st);
+    if (p.big) {
+        const Cut cut = cut_of(tiles_of<MODE>(rows, cols, 64) * batch, tiles_of<MODE>(rows, cols, 128) * batch, k / KB);
+        if (!cut.waves) return product_of<MODE, 2, 2, 2>(A, B, rows, cols, k, batch, fin, SLOTS, cut.splits, partial, st);
+    }
     const auto kernel = ortho_wave_kernel<MODE>;
     if (hipError_t e = ensure_dynamic_lds((const void*)kernel, 131072); e != hipSuccess) return e;
     kernel<<<dim3((unsigned)(tiles_of<MODE>(rows, cols, 64) * batch)), 256, 131072, st>>>(A, B, (int)(k / KB), (int)(rows / 64), (int)(cols / 64), fin);
