@@ -40,7 +40,7 @@ template <class T>
 struct ErrorArgs {
     const T* logits;
     int64_t rows;
-    int C;
+    int C, parts;
     int64_t ld;
     const int* labels;
     const float* weights;
@@ -98,14 +98,18 @@ __device__ __forceinline__ void write_vector(TE* out, int e0, int n, bool whole,
 
 // THREADS threads a row, ROWS rows a work-group (rows of one wave each need no barrier, and a launch of many has fewer work-groups to
 // hand out: 65,536 rows of 1000 bf16 115 us with 256 threads each, 60 with 4 waves for 4 rows). N > 0: N vectors of 16 bytes a thread, kept in
-// registers between reading and writing; 0: a longer row, read a second time.
-template <class T, class TE, int THREADS, int ROWS, int N>
+// registers between reading and writing; 0: a longer row, read a second time. L: as many vectors more in LDS, where registers alone would
+// leave room for one work-group to a CU, whose reading and writing then have nothing beside them.
+template <class T, class TE, int THREADS, int ROWS, int N, int L>
 __global__ __launch_bounds__(THREADS * ROWS) void logit_error_kernel(ErrorArgs<T> a, TE* E) {
+    extern __shared__ u32x4 held[];  // L * THREADS
     static_assert(ROWS == 1 || THREADS == 64, "a row of several waves has the work-group's barrier");
-    __shared__ float2 part[THREADS / 64];
+    __shared__ float2 wave_part[THREADS / 64];
     constexpr int VL = RowType<T>::VL;
     constexpr bool WIDE = sizeof(TE) == 4;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+    // a row's work-groups each read all of it and write a part
+    const int parts = N == 0 ? a.parts : 1, part = N == 0 ? blockIdx.x % a.parts : 0;
+    const int64_t row = N == 0 ? blockIdx.x / a.parts : (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
     if (ROWS > 1 && row >= a.rows) return;
     const T* z = a.logits + row * a.ld;
     TE* out = E ? E + row * a.ldE : nullptr;
@@ -138,18 +142,45 @@ __global__ __launch_bounds__(THREADS * ROWS) void logit_error_kernel(ErrorArgs<T
                 if (FIRST && (unsigned)(y - w0) < 64u * VL) drop_label<T>(reg[i], y - e0);
                 f(reg[i], e0, w0 + 64 * VL <= C);
             }
-        } else {
-            for (int i = 0; i < turns; ++i) {
+        }
+        if constexpr (L > 0) {
+#pragma unroll 1
+            for (int i = N; i < turns; ++i) {
                 const int w0 = i * THREADS * VL + first, e0 = (i * THREADS + tid) * VL;
-                u32x4 v = row_vector(z, e0, C, w0 + 64 * VL <= C);
-                if (FIRST && (unsigned)(y - w0) < 64u * VL) drop_label<T>(v, y - e0);
+                u32x4& v = held[(i - N) * THREADS + tid];
+                if (FIRST && (unsigned)(y - w0) < 64u * VL) {
+                    u32x4 x = v;
+                    drop_label<T>(x, y - e0);
+                    v = x;
+                }
                 f(v, e0, w0 + 64 * VL <= C);
+            }
+        }
+        if constexpr (N == 0) {
+            constexpr int AHEAD = 4;  // vectors of a thread that are read together (those behind the end are -inf, and not written)
+            const int to = FIRST ? turns : turns * (part + 1) / parts;
+#pragma unroll 1
+            for (int i = FIRST ? 0 : turns * part / parts; i < to; i += AHEAD) {
+                u32x4 v[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) v[k] = row_vector(z, ((i + k) * THREADS + tid) * VL, C, (i + k) * THREADS * VL + first + 64 * VL <= C);
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const int w0 = (i + k) * THREADS * VL + first, e0 = ((i + k) * THREADS + tid) * VL;
+                    if (i + k >= to) break;
+                    if (FIRST && (unsigned)(y - w0) < 64u * VL) drop_label<T>(v[k], y - e0);
+                    f(v[k], e0, w0 + 64 * VL <= C);
+                }
             }
         }
     };
     if constexpr (N > 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) reg[i] = row_vector(z, (i * THREADS + tid) * VL, C, i * THREADS * VL + first + 64 * VL <= C);
+    }
+    if constexpr (L > 0) {
+#pragma unroll 4
+        for (int i = N; i < turns; ++i) held[(i - N) * THREADS + tid] = row_vector(z, (i * THREADS + tid) * VL, C, i * THREADS * VL + first + 64 * VL <= C);
     }
     visit(std::true_type{}, [&](const u32x4& v, int, bool) __attribute__((always_inline)) {
         float top = m;
@@ -170,11 +201,11 @@ __global__ __launch_bounds__(THREADS * ROWS) void logit_error_kernel(ErrorArgs<T
     for (int d = 32; d >= 1; d >>= 1) rest += __shfl_xor(rest, d, 64);
     m = top;
     if constexpr (THREADS > 64) {
-        if ((tid & 63) == 0) part[tid >> 6] = float2{m, rest};
+        if ((tid & 63) == 0) wave_part[tid >> 6] = float2{m, rest};
         __syncthreads();
         float2 w[THREADS / 64];
 #pragma unroll
-        for (int i = 0; i < THREADS / 64; ++i) w[i] = part[i];
+        for (int i = 0; i < THREADS / 64; ++i) w[i] = wave_part[i];
 #pragma unroll
         for (int i = 0; i < THREADS / 64; ++i) m = fmaxf(m, w[i].x);
         rest = 0.f;
@@ -182,14 +213,15 @@ __global__ __launch_bounds__(THREADS * ROWS) void logit_error_kernel(ErrorArgs<T
         for (int i = 0; i < THREADS / 64; ++i) rest += w[i].y * exp_diff<WIDE>(w[i].x, m);
     }
     const float ey = exp_diff<true>(zy, m), S = rest + ey;
-    if (a.loss && tid == 0) a.loss[row] = row_loss(rest, ey, zy, m);
+    if (a.loss && tid == 0 && part == 0) a.loss[row] = row_loss(rest, ey, zy, m);
     if (!out) return;
     const float scale = S == 0.f ? 0.f : f / S;
     visit(std::false_type{}, [&](const u32x4& v, int e0, bool whole) __attribute__((always_inline)) {
         write_vector<T>(out, e0, C, whole, v, scale, m);
     });
     // the label's entry, by the thread that has written its vector: after that one's store
-    if (y < C && tid == y / VL % THREADS) out[y] = RowType<TE>::narrow(-scale * rest);
+    const int at_turn = y / (THREADS * VL);
+    if (y < C && tid == y / VL % THREADS && at_turn >= turns * part / parts && at_turn < turns * (part + 1) / parts) out[y] = RowType<TE>::narrow(-scale * rest);
 }
 
 template <int N>
@@ -201,24 +233,32 @@ hipError_t launch(const void* z, int64_t rows, int64_t C, int64_t ld, const int*
     constexpr int VL = RowType<T>::VL;
     for (int64_t r0 = 0; r0 < rows; r0 += LOGIT_LAUNCH_ROWS) {
         const int64_t n = std::min(rows - r0, LOGIT_LAUNCH_ROWS);
-        const ErrorArgs<T> a{(const T*)z + r0 * ld, n, (int)C, ld, labels + r0, weights ? weights + r0 : nullptr, ldE, loss ? loss + r0 : nullptr};
+        // long rows that leave CUs idle are written by several work-groups, unless what one writes is what another reads
+        const int parts = E && E != z ? (int)std::max<int64_t>(1, std::min<int64_t>(8, 256 / n)) : 1;
+        const ErrorArgs<T> a{(const T*)z + r0 * ld, n, (int)C, parts, ld, labels + r0, weights ? weights + r0 : nullptr, ldE, loss ? loss + r0 : nullptr};
         TE* e = E ? (TE*)E + r0 * ldE : nullptr;
-        const auto go = [&](auto threads, auto per, auto vectors) {
-            constexpr int THREADS = decltype(threads)::value, ROWS = decltype(per)::value;
-            logit_error_kernel<T, TE, THREADS, ROWS, decltype(vectors)::value>
-                <<<dim3((unsigned)((n + ROWS - 1) / ROWS)), THREADS * ROWS, 0, st>>>(a, e);
+        const auto go = [&](auto threads, auto per, auto registers, auto more) {
+            constexpr int THREADS = decltype(threads)::value, ROWS = decltype(per)::value, L = decltype(more)::value;
+            const auto kernel = logit_error_kernel<T, TE, THREADS, ROWS, decltype(registers)::value, L>;
+            if (L > 0)
+                if (hipError_t err = ensure_dynamic_lds((const void*)kernel, L * THREADS * 16); err != hipSuccess) return err;
+            const int64_t groups = decltype(registers)::value == 0 ? n * parts : (n + ROWS - 1) / ROWS;
+            kernel<<<dim3((unsigned)groups), THREADS * ROWS, L * THREADS * 16, st>>>(a, e);
+            return hipGetLastError();
         };
+        hipError_t err;
         const int64_t vectors = (C + VL - 1) / VL;
-        if (vectors <= 64) go(I<64>{}, I<4>{}, I<1>{});
-        else if (vectors <= 128) go(I<64>{}, I<4>{}, I<2>{});
-        else if (vectors <= 256) go(I<64>{}, I<4>{}, I<4>{});
-        else if (vectors <= 512) go(I<256>{}, I<1>{}, I<2>{});
-        else if (vectors <= 1024) go(I<256>{}, I<1>{}, I<4>{});
-        else if (vectors <= 4096) go(I<512>{}, I<1>{}, I<8>{});
-        else if (vectors <= 8192) go(I<512>{}, I<1>{}, I<16>{});
-        else if (vectors <= 16384) go(I<1024>{}, I<1>{}, I<16>{});
-        else go(I<1024>{}, I<1>{}, I<0>{});
-        if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
+        if (vectors <= 64) err = go(I<64>{}, I<4>{}, I<1>{}, I<0>{});
+        else if (vectors <= 128) err = go(I<64>{}, I<4>{}, I<2>{}, I<0>{});
+        else if (vectors <= 256) err = go(I<64>{}, I<4>{}, I<4>{}, I<0>{});
+        else if (vectors <= 512) err = go(I<256>{}, I<1>{}, I<2>{}, I<0>{});
+        else if (vectors <= 1024) err = go(I<256>{}, I<1>{}, I<4>{}, I<0>{});
+        else if (vectors <= 4096) err = go(I<512>{}, I<1>{}, I<8>{}, I<0>{});
+        else if (vectors <= 8192) err = go(I<512>{}, I<1>{}, I<16>{}, I<0>{});
+        else if (vectors <= 12800 && rows > 256) err = go(I<512>{}, I<1>{}, I<16>{}, I<9>{});  // two to a CU
+        else if (vectors <= 16384) err = go(I<1024>{}, I<1>{}, I<16>{}, I<0>{});
+        else err = go(I<1024>{}, I<1>{}, I<0>{}, I<0>{});
+        if (err != hipSuccess) return err;
     }
     return hipSuccess;
 }

@@ -237,6 +237,38 @@ def test_logit_error(n, C, pad, dtype, e_dtype):
     _check_error(z + 50.0, y, dtype, w=rng.random(n) * 3 - 1, pad=pad, e_dtype=e_dtype, in_place=dtype == e_dtype)
 
 
+@pytest.mark.parametrize("n,C,dtype", [(300, 33_001, "f32"), (300, 51_200, "f32"), (260, 70_001, "bf16"), (3, 140_001, "bf16"), (40, 70_000, "f32"),
+                                       (257, 131_080, "bf16")])
+def test_logit_error_of_long_rows(n, C, dtype):
+    """Rows that are kept in registers and LDS, or read twice, by one work-group or several."""
+    import torch
+    from paper_2510_02470_amd.binding import logit_error
+
+    g = torch.Generator(device="cuda").manual_seed(C)
+    z = (3 * torch.randn(n, C, generator=g, device="cuda")).to(_tdtype(dtype))
+    y = torch.randint(0, C, (n,), generator=g, device="cuda", dtype=torch.int32)
+    y[0], y[1], y[2] = 0, C - 1, -1
+    w = torch.rand(n, generator=g, device="cuda") + 0.5
+    E, loss = logit_error(z, y, weights=w, dtype=torch.float32)
+    F, loss2 = logit_error(z, y, weights=w)
+    x = z.double()
+    total = torch.logsumexp(x, 1, keepdim=True)
+    p = torch.exp(x - total)
+    i = torch.arange(n, device="cuda")
+    some = (y >= 0).double()
+    want_loss = some * (total[:, 0] - x[i, y.long().clamp(min=0)])
+    p[i, y.long().clamp(min=0)] -= 1.0
+    p *= (w.double() * some)[:, None]
+    # the terms' differences to the maximum are below 40; 32 + C / 512 additions and roundings, and the two sides of p - 1
+    tol = p.abs() * (40 + 8 + 32 + C / 512) * 2.0 ** -24 + 2.0 ** -50
+    assert bool(((E.double() - p).abs() <= tol).all())
+    assert bool(((loss.double() - want_loss).abs() <= want_loss * 2.0 ** -24 + (80 + C / 512) * 2.0 ** -24).all())
+    assert bool(((F.double() - p).abs() <= tol + p.abs() * ref.HALF_STEP[dtype]).all()) and float((loss - loss2).abs().max()) <= 2.0 ** -16
+    in_place = z.clone()
+    H, loss3 = logit_error(in_place, y, weights=w, out=in_place)
+    assert float((H.double() - F.double()).abs().max()) <= 2 * ref.HALF_STEP[dtype] and float((loss3 - loss2).abs().max()) <= 2.0 ** -16
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_logit_error_keeps_the_digits_of_learnt_examples(dtype):
     z, _ = _some_rows(8, 3000, 9)
