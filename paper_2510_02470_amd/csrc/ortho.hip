@@ -7,8 +7,12 @@
 // in the result. So every entry is kept as the sum of two fp16 parts, hi + lo, and hi hi + hi lo + lo hi are summed in fp32: three
 // products on the fp16 matrix cores for one. Two fp16 parts hold 22 bits and more, as fp32 does, where the low part is a normal
 // number; entries are bounded by the largest singular value, whose bound U is known on the host (it follows from the
-// coefficients), so that scaling by a power of two to 2^15 / U leaves entries of 2^-17 U and above that precision and the rest an error
-// of 2^-40 U. (bf16 parts would need three of them, six products.)
+// coefficients), so that scaling by a power of two to 2^14 / U or more leaves entries of 2^-16 U and above that precision and the rest an
+// error of 2^-39 U. (bf16 parts would need three of them, six products.)
+//
+// Matrices of up to 64 x 512 have one work-group each and one launch for all steps (ortho_small_kernel). The others take a launch for
+// each product: by tiles of 256 x 256 (only P X, whose tiles are whole), 128 x 128 or 64 x 64, whichever fills the chip (cut_of).
+// 4096 x 4096, five steps: 4.0 ms, 1.03 PFLOP/s of the products that symmetry leaves (the library's plain fp16 product of that size: 1.04).
 //
 // Layout: 32 columns of a row are 128 bytes, their 32 hi parts and then their 32 lo parts; rows and columns are padded with zeros to
 // multiples of the tiles' side. X is kept row by row for A and column by column for P X: the instructions take both factors along the
@@ -390,8 +394,9 @@ __global__ __launch_bounds__(WR * WC * 64) void ortho_product_kernel(Parts A, Pa
 }
 
 // The same for few tiles: 64 x 64, all of it by each of four waves, which take the blocks of the summed index in turn and add up what
-// they have in the end. A wave has its own ring of two blocks and waits for nobody. (Four waves with a quarter of the tile each read
-// twice as much from LDS as the matrix cores can use: 1000 x 2049, A 21 us with them and XX so.)
+// they have in the end. A wave has its own ring of two blocks and waits for nobody. Bound by LDS: four blocks are 64 KB written there (450 ns
+// from an L2) and 64 KB read (390 ns) for matrix instructions of 390 ns; a turn takes 1.0 us. (With a quarter of the tile each, four waves
+// read twice as much for a block: X X' of 1000 x 2049 in 21 us instead of 17, P in 14 instead of 12.)
 template <int MODE>
 __global__ __launch_bounds__(256) void ortho_wave_kernel(Parts A, Parts B, int kblocks, int tiles_r, int tiles_c, Finish fin) {
     constexpr int STAGE = 128 * 8, LOADS = 16, KS = 4;
@@ -522,6 +527,9 @@ __global__ __launch_bounds__(64) void ortho_join_kernel(const f32x4* __restrict_
 
 // ---- small matrices ---------------------------------------------------------------------------------------------
 
+// (64 x 256, five steps: 35 us, 95 with a launch for each product; a step takes 5: 2.2 of matrix instructions, the rest is three
+// meetings of the work-group and what each wave does between them on its own; 43 us with 64 columns a wave, which is what more than 256
+// columns take: 70 for 64 x 512. Longer rows do not fit in registers.)
 constexpr int SMALL_M = 64, SMALL_N = 512, MAX_STEPS = 32;
 
 // What the steps of a call need, for any matrix of it.
@@ -536,12 +544,12 @@ struct Steps {
     } at[MAX_STEPS];
 };
 
-// Up to 64 x 512 (m <= n), all steps by one work-group, which keeps X in registers: each wave has 64 columns of it, once with a lane for a
+// Up to 64 x 512 (m <= n), all steps by one work-group, which keeps X in registers: each wave has CW blocks of 32 columns of it, once with a lane for a
 // row (as X X^T takes it) and once with a lane for a column (as P X takes it). The instruction leaves a lane with four consecutive
 // entries along the other side, and two halves of a wave swap registers to make eight of them: P X is formed both ways, X P' and P X, in
-// place of a transposition through LDS. A is summed over the waves in LDS. WAVES: at most; four may have the registers of eight.
-template <class T, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int rows, int cols, int64_t ld, int64_t stride, T* out, int64_t ld_out,
+// place of a transposition through LDS. A is summed over the waves in LDS.
+template <class T, int CW>
+__global__ __launch_bounds__(512) void ortho_small_kernel(const T* G, int rows, int cols, int64_t ld, int64_t stride, T* out, int64_t ld_out,
                                                           int64_t stride_out, Steps p) {
     extern __shared__ u32x4 lds[];
     __shared__ double norms[8];
@@ -550,20 +558,27 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
     const int l32 = lane & 31, h = lane >> 5;
     const bool tall = rows > cols;
     const int m = tall ? cols : rows, n = tall ? rows : cols;
-    const int c0 = wave * 64, used = (n + 63) >> 6;  // waves behind the last column only help with A and P
+    constexpr int XN = 32 * CW;  // columns of a wave, and loads of a lane
+    const int c0 = wave * XN, used = (n + XN - 1) / XN;  // waves behind the last column only help with A and P
     const bool mine = wave < used;
 
-    // the wave's 64 x 64 entries, coalesced; scaled and split they go through LDS to the lanes that have them as factors
+    // the wave's 64 rows of XN entries, coalesced; scaled and split they go through LDS to the lanes that have them as factors
     const T* g = G + (int64_t)blockIdx.x * stride;
-    float x[64];
+    float x[XN];
+    auto place = [&](int i, int& r, int& c) __attribute__((always_inline)) {
+        r = tall ? lane : CW == 2 ? i : 2 * i + h;
+        c = tall ? i : CW == 2 ? lane : l32;
+    };
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
-        const int r = tall ? lane : i, c = c0 + (tall ? i : lane);
+    for (int i = 0; i < XN; ++i) {
+        int r, c;
+        place(i, r, c);
+        c += c0;
         x[i] = r < m && c < n ? RowType<T>::widen(tall ? g[(int64_t)c * ld + r] : g[(int64_t)r * ld + c]) : 0.f;
     }
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 64; ++i) s = __builtin_fma((double)x[i], (double)x[i], s);
+    for (int i = 0; i < XN; ++i) s = __builtin_fma((double)x[i], (double)x[i], s);
     for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
     if (lane == 0) norms[wave] = s;
     __syncthreads();
@@ -573,35 +588,37 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
     const double inv = s > 0.0 || s != s ? p.sx / (sqrt(s) + p.eps) : 0.0;
     const int power = ilogb(inv == 0.0 ? 1.0 : inv);
     const float rest = (float)ldexp(inv, -power);
-    uint32_t* xs = (uint32_t*)lds + wave * (64 * 65);
+    uint32_t* xs = (uint32_t*)lds + wave * (64 * (XN + 1));
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
+    for (int i = 0; i < XN; ++i) {
+        int r, c;
+        place(i, r, c);
         f16 hi, lo;
         split(ldexpf(x[i], power) * rest, hi, lo);
-        xs[(tall ? lane : i) * 65 + (tall ? i : lane)] = (uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
+        xs[r * (XN + 1) + c] = (uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
     }
-    f16x8 by_row[2][4][2], by_col[2][4][2];  // [32 rows or columns][16 of the others][high, low]
+    auto gather = [&](f16x8* to, int r, int c, int down) __attribute__((always_inline)) {  // eight entries from (r, c) on, along a row or down a column
+        u32x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t u[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) u[q] = xs[(r + (down ? 2 * e + q : 0)) * (XN + 1) + c + (down ? 0 : 2 * e + q)];
+            hi[e] = (u[0] & 0xFFFFu) | u[1] << 16;
+            lo[e] = u[0] >> 16 | (u[1] & 0xFFFF0000u);
+        }
+        to[0] = __builtin_bit_cast(f16x8, hi);
+        to[1] = __builtin_bit_cast(f16x8, lo);
+    };
+    f16x8 by_row[2][2 * CW][2], by_col[CW][4][2];  // [32 rows or columns][16 of the others][high, low]
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 2 * CW; ++k) gather(by_row[i][k], 32 * i + l32, 16 * k + 8 * h, 0);
 #pragma unroll
-            for (int way = 0; way < 2; ++way) {
-                u32x4 hi, lo;
+    for (int j = 0; j < CW; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t u[2];
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int along = 16 * k + 8 * h + 2 * e + q, across = 32 * i + l32;
-                        u[q] = xs[way ? along * 65 + across : across * 65 + along];
-                    }
-                    hi[e] = (u[0] & 0xFFFFu) | u[1] << 16;
-                    lo[e] = u[0] >> 16 | (u[1] & 0xFFFF0000u);
-                }
-                (way ? by_col : by_row)[i][k][0] = __builtin_bit_cast(f16x8, hi);
-                (way ? by_col : by_row)[i][k][1] = __builtin_bit_cast(f16x8, lo);
-            }
+        for (int k = 0; k < 4; ++k) gather(by_col[j][k], 16 * k + 8 * h, 32 * j + l32, 1);
     __syncthreads();
 
     f32x4* const sums = (f32x4*)lds;               // per wave three blocks of 32 x 32 of X X^T: (0, 0), (1, 0), (1, 1)
@@ -655,7 +672,7 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
         if (mine) {
             f32x16 acc[3] = {zero, zero, zero};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 2 * CW; ++k) {
                 const auto three = [&](auto one) __attribute__((always_inline)) {
                     one(acc[0], by_row[0][k], by_row[0][k]);
                     one(acc[1], by_row[1][k], by_row[0][k]);
@@ -714,7 +731,7 @@ __global__ __launch_bounds__(WAVES * 64) void ortho_small_kernel(const T* G, int
         T* const to = out + (int64_t)blockIdx.x * stride_out;
         if (!mine) continue;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {  // 32 columns
+        for (int j = 0; j < CW; ++j) {  // 32 columns
             f32x16 down[2] = {zero, zero}, along[2] = {zero, zero};  // P X: a lane has a column; X' P: a lane has a row
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -786,9 +803,11 @@ struct Plan {
 int64_t padded(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
-// tiles of 128 x 128 of X, from which on they are used
+// Tiles of 128 x 128 of X from which on its sides are padded to them (fewer leave most CUs idle, and the padding costs: with 60 and 200 the
+// sizes in between take the same time within 3%), and of 256 x 256 for P X, which keep 256 CUs busy once (4096 x 4096: 385 us in tiles of 128,
+// 341 so; fewer leave CUs idle, for a tile takes its 341 us alone as well).
 constexpr int64_t BIG_FROM = 100;
-constexpr int64_t HUGE_FROM = 224;    // ... of 256 x 256
+constexpr int64_t HUGE_FROM = 224;
 constexpr int64_t SLOTS = 512;        // work-groups of 128 x 128 at a time, two to a CU
 constexpr int SPLIT_BLOCKS = 8;       // blocks of the summed index in a part of it, at least
 constexpr int64_t JOIN_BYTES = SLOTS * 128 * 128 * 4;
@@ -938,11 +957,12 @@ hipError_t run(const Plan& p, const T* G, int64_t batch, int64_t rows, int64_t c
             U = next;
             sx = sn;
         }
-        // (a few matrices have four waves each for what is not split over columns)
-        const int waves = std::max((int)(p.n + 63) / 64, batch <= 512 ? 4 : 1);
-        const auto bytes = [](int w) { return std::max(w * 64 * 65 * 4, w * 12288 + 32768); };
-        const auto kernel = waves <= 4 ? ortho_small_kernel<T, 4> : ortho_small_kernel<T, 8>;
-        if (hipError_t e = ensure_dynamic_lds((const void*)kernel, bytes(waves <= 4 ? 4 : 8)); e != hipSuccess) return e;
+        // (a few matrices have four waves each, at least, for what is not split over columns)
+        const bool wide = p.n > 256;
+        const int waves = std::max((int)(p.n + (wide ? 63 : 31)) / (wide ? 64 : 32), batch <= 512 ? 4 : 1);
+        const auto bytes = [&](int w) { return std::max(w * 64 * (wide ? 65 : 33) * 4, w * 12288 + 32768); };
+        const auto kernel = wide ? ortho_small_kernel<T, 2> : ortho_small_kernel<T, 1>;
+        if (hipError_t e = ensure_dynamic_lds((const void*)kernel, bytes(8)); e != hipSuccess) return e;
         kernel<<<dim3((unsigned)batch), waves * 64, bytes(waves), st>>>(G, (int)rows, (int)cols, ld, stride, out, ld_out, stride_out, q);
         return hipGetLastError();
     }

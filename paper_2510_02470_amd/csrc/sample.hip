@@ -4,6 +4,13 @@
 // addition, so that the label is a function of the row and its number alone, however a row is cut over threads; a weight is
 // off by at most 2^-43 of the greatest, which moves the borders between the classes of a row of 2^20 by less than 2^-23 of
 // it at worst and by 2^-33 as such errors fall out. Everything up to the comparison is done in 64 bits.
+//
+// A row has one work-group (a wave up to 256 vectors of 16 bytes, four up to 1024, sixteen up to 4096, from LDS; longer rows are read again
+// by every pass, 8 waves twice on a CU, or 16 where there are no more than 256 rows). Passes: the maximum; for top-k a histogram of the
+// distance to it, and a list of all that is in the K-th's bin and above, on which the rest is done; for top-p without it an approximate
+// histogram of weights and one exact pass; otherwise one exact pass. An exact pass is bound by 64-bit arithmetic: 18 such instructions
+// and about as many others a class, 30 us for a row of 131,072 on a CU, where a reading takes 10. 1024 rows of 131,072 bf16: the greatest 84 us,
+// top-k 50 141, plain 210, top-p 0.9 at 1.0 318 to 420 (as peaked as the rows are).
 #include <algorithm>
 #include <type_traits>
 
@@ -332,11 +339,9 @@ __device__ __forceinline__ int locate(const Row<T, THREADS, STAGED>& r, Shared<T
 // The bins of a histogram: equal parts of the distance to the maximum, everything beyond `range` in the last.
 struct Bins {
     float m, scale, last;
-    __device__ Bins(float m_, float range, int bins) : m(m_), scale((float)(bins - 1) / range), last((float)(bins - 1)) {}
-    __device__ int operator()(float x) const {  // (scale may be infinite: then only the maximum is in bin 0)
-        const float d = m - x;
-        return d > 0.f ? (int)fminf(d * scale, last) : 0;
-    }
+    // (a range of 0 would make 0 * infinity of the maximum's distance)
+    __device__ Bins(float m_, float range, int bins) : m(m_), scale(fminf((float)(bins - 1) / range, 1e30f)), last((float)(bins - 1)) {}
+    __device__ __forceinline__ int operator()(float x) const { return (int)fminf((m - x) * scale, last); }
 };
 
 // The least value whose bin is at most b (bins fall with the value).
@@ -593,7 +598,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
         clear_histogram(S, r.tid);
         r.each([&](float x, int) __attribute__((always_inline)) {
             // (whole numbers: adding floats in LDS takes ten times as long)
-            const uint32_t w = (uint32_t)(__builtin_amdgcn_exp2f((x - m) * c2) * 0x1p31f);
+            const uint32_t w = (uint32_t)__builtin_amdgcn_exp2f(fmaf(x - m, c2, 31.f));
             if (w) atomicAdd((unsigned long long*)&S.hist[bins(x)], (unsigned long long)w);
         });
         __syncthreads();
