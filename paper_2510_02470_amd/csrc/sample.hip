@@ -85,8 +85,13 @@ struct Shared {
     uint64_t seg[SEGS];   // sums of segments
     uint64_t part[W];
     float fpart[2 * W];
-    uint64_t lkey[LIST], skey[LIST];  // of listed classes key and place, one number in their common order
-    uint64_t lw[LIST], sw[LIST];      // and weight
+    union {
+        struct {
+            uint64_t lkey[LIST], skey[LIST];  // of listed classes key and place, one number in their common order
+            uint64_t lw[LIST], sw[LIST];      // and weight
+        };
+        uint64_t table[4 * LIST];  // weights by value (draw_by_value)
+    };
     uint64_t found[2];
     unsigned listed, few;
     uint64_t answer;
@@ -226,10 +231,10 @@ __device__ __forceinline__ uint64_t share_of(float u, uint64_t total) {
     return t >= total ? total - 1 : t;
 }
 
-// The first of `count` sums in LDS up to which they come to more than t = want(their total): its number, and in S.found the sum of
-// those before it and its own.
+// The first of `count` sums (sums[i], of LDS) up to which they come to more than t = want(their total): its number, and in S.found the
+// sum of those before it and its own.
 template <int THREADS, class E, class F>
-__device__ __forceinline__ int find_sum(Shared<THREADS>& S, const E* sums, int count, int tid, uint64_t& total, F want) {
+__device__ __forceinline__ int find_sum(Shared<THREADS>& S, E sums, int count, int tid, uint64_t& total, F want) {
     const int per = (count + THREADS - 1) / THREADS;
     uint64_t own = 0;
     for (int i = 0; i < per; ++i)
@@ -264,16 +269,12 @@ __device__ __forceinline__ int find_sum(Shared<THREADS>& S, const E* sums, int c
     return (int)S.listed;
 }
 
-// With the sums of segments in LDS: the element at which the sum of f (value, element) passes t, the sum of all being total.
+// The element of a segment at which the sum of f (value, element) passes t, `before` being the sum before the segment.
 template <class T, int THREADS, bool STAGED, class F>
-__device__ __forceinline__ int locate_in(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t& total, const float* u, uint64_t t0, F f) {
+__device__ __forceinline__ int locate_at(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, int seg, uint64_t before, uint64_t t, F f) {
     constexpr int VL = RowType<T>::VL, W = THREADS / 64;
     const int lane = r.tid & 63, wave = r.tid >> 6;
-    const int seg = find_sum<THREADS>(S, S.seg, r.count * W, r.tid, total,
-                                      [&](uint64_t all) { return u ? share_of(*u, all) : t0; });
-    const uint64_t t = u ? share_of(*u, total) : t0;
     if (wave == seg % W) {
-        uint64_t before = S.found[0];
         bool done = false;
 #pragma unroll 1
         for (int q = 0; q < U; ++q) {
@@ -304,6 +305,14 @@ __device__ __forceinline__ int locate_in(const Row<T, THREADS, STAGED>& r, Share
     }
     __syncthreads();
     return (int)S.answer;
+}
+
+// With the sums of segments in LDS: the element at which the sum of f (value, element) passes t, the sum of all being total.
+template <class T, int THREADS, bool STAGED, class F>
+__device__ __forceinline__ int locate_in(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t& total, const float* u, uint64_t t0, F f) {
+    const int seg = find_sum<THREADS>(S, (const uint64_t*)S.seg, r.count * r.W, r.tid, total,
+                                      [&](uint64_t all) { return u ? share_of(*u, all) : t0; });
+    return locate_at(r, S, seg, S.found[0], u ? share_of(*u, total) : t0, f);
 }
 
 // The same from the row alone. keeps(value, element): f is not 0; bits(value, element): f, and ROUND_BITS if `rounded`, for what is kept.
@@ -410,7 +419,7 @@ __device__ __forceinline__ Cut front(const Row<T, THREADS, STAGED>& r, Shared<TH
         });
         __syncthreads();
         uint64_t total;
-        const int b = find_sum<THREADS>(S, S.hist, S.BINS, r.tid, total, [&](uint64_t) { return t - above; });
+        const int b = find_sum<THREADS>(S, (const uint64_t*)S.hist, S.BINS, r.tid, total, [&](uint64_t) { return t - above; });
         above += S.found[0];
         if (shift == 33) {
             from = least_of_bin(bins, b - 1);
@@ -483,7 +492,7 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
             if (S.lkey[i] >= last) atomicAdd((unsigned long long*)&S.hist[bins(value(i))], (unsigned long long)S.lw[i]);
         __syncthreads();
         uint64_t t = 0;
-        const int at = find_sum<THREADS>(S, S.hist, S.BINS, tid, total, [&](uint64_t all) {
+        const int at = find_sum<THREADS>(S, (const uint64_t*)S.hist, S.BINS, tid, total, [&](uint64_t all) {
             const double q = ceil((double)P * (double)all);
             return t = q >= 1.0 ? (uint64_t)q - 1 : 0;
         });
@@ -500,11 +509,149 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
     for (int i = tid; i < count; i += THREADS)
         if (kept(i)) atomicAdd((unsigned long long*)&S.seg[r.segment_of(place(i))], (unsigned long long)S.lw[i]);
     __syncthreads();
-    const int seg = find_sum<THREADS>(S, S.seg, r.count * r.W, tid, total, [&](uint64_t all) { return share_of(u, all); });
+    const int seg = find_sum<THREADS>(S, (const uint64_t*)S.seg, r.count * r.W, tid, total, [&](uint64_t all) { return share_of(u, all); });
     const uint64_t base = S.found[0];
     return (int)~(uint32_t)passing(S, count, tid, base, share_of(u, total),
                                    [&](int i) __attribute__((always_inline)) { return kept(i) & (r.segment_of(place(i)) == seg); },
                                    [&](int i) __attribute__((always_inline)) { return (uint64_t)(uint32_t)S.lkey[i]; }, weight);
+}
+
+// ---- long bf16 rows without top-k -------------------------------------------------------------------------------
+
+// A bf16 of magnitude 2^-9 to 2^7 is one of 4096 values, and a long row has few of them, each many times. One pass counts them; weights,
+// the border of top-p and what min-p leaves are found from values and counts (with 4096 exponentials instead of one for every class), and
+// a second pass adds up a table's entries: 10 instructions a class and a reading of LDS instead of 36. Smaller magnitudes, one in a
+// thousand, are listed; a row with more of them, or with greater ones that matter, is left to the other passes.
+constexpr int VALUES = 4096, HALF = VALUES / 2, MAX_TINY = 1024;
+constexpr unsigned VALUES_FROM = 118u << 7;  // 2^-9
+
+__device__ __forceinline__ unsigned bits_of(const u32x4& v, int k) { return k & 1 ? v[k >> 1] >> 16 : v[k >> 1] & 0xFFFFu; }
+// (in falling order)
+__device__ __forceinline__ unsigned number_of(unsigned bits, unsigned above) { return bits >> 15 ? HALF + above : HALF - 1 - above; }
+__device__ __forceinline__ unsigned value_bits(int i) { return i < HALF ? VALUES_FROM + (HALF - 1 - i) : 0x8000u + VALUES_FROM + (i - HALF); }
+__device__ __forceinline__ float bf16_value(unsigned bits) { return __uint_as_float(bits << 16); }
+
+// The sums of the values, those of small magnitude as one in the middle.
+struct ValueSums {
+    const uint32_t* counts;
+    const uint64_t* table;
+    uint64_t tiny;
+    __device__ __forceinline__ uint64_t operator[](int i) const {
+        if (i == HALF) return tiny;
+        const int n = i - (i > HALF);
+        return counts[n] * table[n];
+    }
+};
+// Sums of a segment: of weights below, of classes at the border from this bit on (1024 classes of up to 2^42).
+constexpr int AT_BORDER = 53;
+struct BorderCounts {
+    const uint64_t* seg;
+    __device__ __forceinline__ uint64_t operator[](int i) const { return seg[i] >> AT_BORDER; }
+};
+
+// The label, m and the total; or -1: a row for the other passes.
+template <class T, int THREADS, bool STAGED>
+__device__ __forceinline__ int draw_by_value(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, double inv, float P, double border, float u,
+                                             float& m, uint64_t& total) {
+    constexpr int VL = RowType<T>::VL, W = THREADS / 64, SEGMENTS = SAGE_MAX_CLASSES / (64 * U * VL);
+    static_assert(VL == 8 && 64 * U * VL <= 1024 && Shared<THREADS>::BINS * 2 >= VALUES && Shared<THREADS>::LIST * 4 >= VALUES, "room in LDS");
+    static_assert(SEGMENTS + MAX_TINY / 2 <= Shared<THREADS>::SEGS, "room behind the segments");
+    const int tid = r.tid;
+    uint32_t* const counts = (uint32_t*)S.hist;
+    uint32_t* const tiny = (uint32_t*)(S.seg + SEGMENTS);
+    if (tid == 0) S.few = 0;
+    clear_histogram(S, tid);
+    float low = -INFINITY;  // greatest of the values below all counted ones
+    bool other = false;     // NaN, or above all counted ones
+    r.template visit<true>([&](int, const u32x4* v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+#pragma unroll
+            for (int k = 0; k < VL; ++k) {
+                if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                const unsigned h = bits_of(v[q], k), above = (h & 0x7FFFu) - VALUES_FROM;
+                if (above < (unsigned)HALF) {
+                    atomicAdd(&counts[number_of(h, above)], 1u);
+                } else if ((int)above >= 0) {
+                    if (h >> 15 && h <= 0xFF80u) low = fmaxf(low, bf16_value(h));
+                    else other = true;
+                } else {
+                    const unsigned p = atomicAdd(&S.few, 1u);
+                    if (p < (unsigned)MAX_TINY) tiny[p] = h;
+                }
+            }
+        }
+    });
+    low = group_reduce<THREADS>(other ? INFINITY : low, S.fpart, [](float a, float b) { return fmaxf(a, b); });
+    constexpr int PER = VALUES / THREADS;
+    float first = VALUES;
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i)
+        if (counts[tid * PER + i]) first = (float)(tid * PER + i);
+    first = group_reduce<THREADS>(first, S.fpart + W, [](float a, float b) { return fminf(a, b); });
+    const int few = (int)S.few;
+    if (low == INFINITY || first == (float)VALUES || few > (first < (float)HALF ? MAX_TINY : 0)) return -1;
+    m = bf16_value(value_bits((int)first));
+    const double md = m;
+    if (((double)low - md) * inv > -29.9) return -1;  // (below -43 ln 2 there is no weight)
+    auto weight = [&](float x) __attribute__((always_inline)) { return weight_of(((double)x - md) * inv); };
+    for (int i = tid; i < VALUES; i += THREADS) S.table[i] = counts[i] ? weight(bf16_value(value_bits(i))) : 0;
+    uint64_t tiny_sum = 0;
+    for (int i = tid; i < few; i += THREADS) tiny_sum += weight(bf16_value(tiny[i]));
+    tiny_sum = group_sum<THREADS>(tiny_sum, S);  // (the table is there too)
+    int last = VALUES;         // the last value that top-p keeps any of
+    uint64_t kept = 0, at_last = 0;  // so many, if not all of it, of this weight
+    if (P < 1.f) {
+        uint64_t t = 0;
+        const int at = find_sum<THREADS>(S, ValueSums{counts, S.table, tiny_sum}, VALUES + 1, tid, total, [&](uint64_t all) {
+            const double q = ceil((double)P * (double)all);
+            return t = q >= 1.0 ? (uint64_t)q - 1 : 0;
+        });
+        if (at == HALF) return -1;
+        last = at - (at > HALF);
+        at_last = S.table[last];
+        kept = (t - S.found[0]) / at_last + 1;
+        if (kept >= counts[last]) kept = 0;
+    }
+    const float value = last < VALUES ? bf16_value(value_bits(last)) : -INFINITY;
+    __syncthreads();
+    // what is left of the table; a value kept in part is counted
+    for (int i = tid; i < VALUES; i += THREADS) {
+        if (i == last && kept) S.table[i] = 1ull << AT_BORDER;
+        else if (i > last || (double)bf16_value(value_bits(i)) - md < border) S.table[i] = 0;
+    }
+    if ((double)value - md < border) at_last = 0;
+    const bool tiny_kept = last >= HALF;
+    auto drawn = [&](float x) __attribute__((always_inline)) { return weight(x) & mask_of((double)x - md >= border); };
+    __syncthreads();
+    r.visit([&](int i, const u32x4* v) __attribute__((always_inline)) {
+        uint64_t own = 0;
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+#pragma unroll
+            for (int k = 0; k < VL; ++k) {
+                if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                const unsigned h = bits_of(v[q], k), above = (h & 0x7FFFu) - VALUES_FROM;
+                if (above < (unsigned)HALF) own += S.table[number_of(h, above)];
+                else if (tiny_kept && (int)above < 0) own += drawn(bf16_value(h));
+            }
+        }
+        const uint64_t s = wave_sum(own);
+        if ((tid & 63) == 0) S.seg[i * W + (tid >> 6)] = s;
+    });
+    __syncthreads();
+    Cut cut{value, 0x7FFFFFFF};
+    if (kept) {
+        const int seg = find_sum<THREADS>(S, BorderCounts{S.seg}, r.count * W, tid, total, [&](uint64_t) { return kept - 1; });
+        const uint64_t before = S.found[0];
+        cut.place = 1 + locate_at(r, S, seg, before, kept - 1, [&](float x, int) __attribute__((always_inline)) { return x == value ? 1ull : 0ull; });
+        for (int i = tid; i < r.count * W; i += THREADS) {
+            const uint64_t s = S.seg[i], n = i < seg ? s >> AT_BORDER : i == seg ? kept - before : 0;
+            S.seg[i] = (s & ((1ull << AT_BORDER) - 1)) + n * at_last;
+        }
+        __syncthreads();
+    }
+    return locate_in(r, S, total, &u, 0, [&](float x, int e) __attribute__((always_inline)) { return drawn(x) & mask_of(cut.keeps(x, e)); });
 }
 
 template <class T, int THREADS, bool STAGED>
@@ -521,6 +668,23 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
     const int K = how.top_k_rows ? how.top_k_rows[row] : how.top_k;
     const float u = u_rows[row];
 
+    auto done = [&](int j, float m, double inv, uint64_t total) __attribute__((always_inline)) {
+        if (r.tid != 0) return;
+        labels[row] = j;
+        if (logp) logp[row] = (float)(((double)RowType<T>::widen(r.z[j]) - (double)m) * inv - log((double)total * 0x1p-42));
+    };
+    const double inv = 1.0 / (double)T32;
+    double border = -INFINITY;  // z - m of the least class that min-p keeps
+    if (M32 > 0.f) border = (double)T32 * log((double)fminf(M32, 1.f));
+    if constexpr (sizeof(T) == 2 && THREADS >= 512) {
+        if (T32 > 0.f && !(K > 0 && K < C)) {
+            float m;
+            uint64_t total = 0;
+            const int j = draw_by_value(r, S, inv, P32, border, u, m, total);
+            if (j >= 0) return done(j, m, inv, total);
+            __syncthreads();
+        }
+    }
     float m = -INFINITY, low = INFINITY;  // greatest, and least finite
     bool nan = false;
     r.template each<true>([&](float x, int) __attribute__((always_inline)) {
@@ -548,12 +712,10 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
         }
         return;
     }
-    const double Td = T32, inv = 1.0 / Td, md = m;
+    const double md = m;
     const float spread = fminf(m - low, 3e38f);
     auto bits = [&](float x) __attribute__((always_inline)) { return weight_bits(((double)x - md) * inv); };
     auto weight = [&](float x, int) __attribute__((always_inline)) { return bits(x) - ROUND_BITS; };
-    double border = -INFINITY;  // z - m of the least class that min-p keeps
-    if (M32 > 0.f) border = Td * log((double)fminf(M32, 1.f));
     Cut cut{-INFINITY, 0};  // (-inf has no weight)
     if (K > 0 && K < C) {
         // the bin that the K-th is in; if all up to it can be listed, the rest is done on the list
@@ -565,7 +727,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
         });
         __syncthreads();
         uint64_t all;
-        const int b = find_sum<THREADS>(S, counts, S.BINS, r.tid, all, [&](uint64_t) { return (uint64_t)K - 1; });
+        const int b = find_sum<THREADS>(S, (const uint32_t*)counts, S.BINS, r.tid, all, [&](uint64_t) { return (uint64_t)K - 1; });
         const uint64_t before = S.found[0], through = before + S.found[1];
         if (all <= (uint64_t)K) {
             // every class that has a weight is among the first K
@@ -602,7 +764,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
             if (w) atomicAdd((unsigned long long*)&S.hist[bins(x)], (unsigned long long)w);
         });
         __syncthreads();
-        const int b = find_sum<THREADS>(S, S.hist, S.BINS, r.tid, total, [&](uint64_t all) { return share_of(P32, all); });
+        const int b = find_sum<THREADS>(S, (const uint64_t*)S.hist, S.BINS, r.tid, total, [&](uint64_t all) { return share_of(P32, all); });
         __syncthreads();
         if (r.tid == 0) S.listed = 0;
         __syncthreads();
@@ -666,10 +828,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
     if (j < 0)
         j = locate(r, S, total, &u, 0,
                    [&](float x, int e) __attribute__((always_inline)) { return ((double)x - md >= border) & cut.keeps(x, e) & (e < C); }, weight);
-    if (r.tid == 0) {
-        labels[row] = j;
-        if (logp) logp[row] = (float)(((double)RowType<T>::widen(r.z[j]) - md) * inv - log((double)total * 0x1p-42));
-    }
+    done(j, m, inv, total);
 }
 
 template <class T>

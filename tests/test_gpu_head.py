@@ -126,6 +126,50 @@ def test_sample_borders_among_many_classes(n, C, dtype):
         _check_sample(z, u, dtype, **how)
 
 
+def _rows_of_values(kind, n, C, rng):
+    """Long rows whose values repeat, or are of magnitudes that only some rows have."""
+    z = 2.0 * rng.standard_normal((n, C))
+    some = lambda count: (np.arange(n)[:, None], np.stack([rng.permutation(C)[:count] for _ in range(n)]))
+    if kind == "few values":
+        z = rng.integers(-4, 5, size=(n, C)) + 0.5
+    elif kind == "one value":
+        z = np.repeat(np.resize([0.5, -3.0, 0.0, 130.0], n)[:, None], C, axis=1)
+    elif kind == "whole numbers":
+        z = np.round(z)  # zeros among them
+    elif kind == "some near zero":
+        z[some(300)] = 0.001 * rng.standard_normal((n, 300))
+    elif kind == "near zero":
+        z *= 0.0005
+    elif kind == "most weight near zero":
+        z = -6.0 + 0.1 * z
+        z[some(700)] = 0.001 * rng.standard_normal((n, 700))
+        z[some(3)] = 1.0
+    elif kind == "negative":
+        z = -1.0 - np.abs(z)
+    elif kind == "great":
+        z[some(4)] = 127.0 + 4.0 * rng.random((n, 4))
+    elif kind == "far below":
+        z[some(C // 2)] = np.resize([-128.0, -150.0, -3.3e38, -np.inf], n)[:, None]
+    elif kind == "no distribution":
+        z[np.arange(n), rng.integers(0, C, size=n)] = np.resize([np.nan, np.inf, -np.inf], n)
+    return z
+
+
+@pytest.mark.parametrize("kind", ["few values", "one value", "whole numbers", "some near zero", "near zero", "most weight near zero", "negative",
+                                  "great", "far below", "no distribution"])
+@pytest.mark.parametrize("n,C", [(8, 9001), (8, 40_000), (260, 33_001)])
+def test_sample_values_of_long_rows(n, C, kind):
+    rng = np.random.default_rng(C)
+    z = _rows_of_values(kind, n, C, rng)
+    u = rng.random(n, dtype=np.float32)
+    for dtype in ("bf16", "f32") if n < 100 else ("bf16",):
+        _check_sample(z, u, dtype, pad=3, rows_as_tensors=True, temperature=np.resize([1.0, 0.5, 30.0, 1.0, math.inf, 2.0, 1e-40], n),
+                      top_p=np.resize([0.9, 1.0, 0.3, 0.02, 0.6], n), min_p=np.resize([0.0, 0.0, 0.0, 0.1], n), top_k=np.resize([0, C, 0], n))
+    if n < 100:
+        for p in (0.0, 0.05, 0.5, 0.97):
+            _check_sample(z, u, "bf16", top_p=p)
+
+
 def test_sample_random_numbers_at_and_beyond_the_ends():
     z, _ = _some_rows(8, 500, 3)
     z[:, 490:] = -np.inf  # the last class with a weight is not the last class
