@@ -9,8 +9,9 @@
 // by every pass, 8 waves twice on a CU, or 16 where there are no more than 256 rows). Passes: the maximum; for top-k a histogram of the
 // distance to it, and a list of all that is in the K-th's bin and above, on which the rest is done; for top-p without it an approximate
 // histogram of weights and one exact pass; otherwise one exact pass. An exact pass is bound by 64-bit arithmetic: 18 such instructions
-// and about as many others a class, 30 us for a row of 131,072 on a CU, where a reading takes 10. 1024 rows of 131,072 bf16: the greatest 84 us,
-// top-k 50 141, plain 210, top-p 0.9 at 1.0 318 to 420 (as peaked as the rows are).
+// and about as many others a class, 30 us for a row of 131,072 on a CU, where a reading takes 10. So long bf16 rows without top-k are
+// counted by value, in two passes (draw_by_value). 1024 rows of 131,072 bf16: the greatest 85 us, top-k 50 136, plain 155 (214 by classes),
+// top-p 0.9 159 (410); 37 rows of 50,021 bf16 28 and 34 (31 and 52). A row that has to be left to the other passes costs 7% more.
 #include <algorithm>
 #include <type_traits>
 
@@ -138,7 +139,7 @@ struct Row {
             for (int u = 0; u < U; ++u) v[u] = fetch(place(i, u));
         }
     }
-    // f(segment of the wave, vectors); first: the pass that reads the row
+    // f(segment of the wave, vectors), the last one if it says false; first: the pass that reads the row
     template <bool FIRST = false, class F>
     __device__ __forceinline__ void visit(F f) const {
         if constexpr (STAGED && !FIRST) {
@@ -160,7 +161,11 @@ struct Row {
 #pragma unroll
                     for (int u = 0; u < U; ++u) lds[(i * U + u) * THREADS + tid] = v[u];
                 }
-                f(i, v);
+                if constexpr (std::is_same<decltype(f(i, v)), bool>::value) {
+                    if (!f(i, v)) break;
+                } else {
+                    f(i, v);
+                }
 #pragma unroll
                 for (int u = 0; u < U; ++u) v[u] = next[u];
             }
@@ -581,6 +586,7 @@ __device__ __forceinline__ int draw_by_value(const Row<T, THREADS, STAGED>& r, S
                 }
             }
         }
+        return (int)__builtin_amdgcn_readfirstlane(*(volatile unsigned*)&S.few) <= MAX_TINY;
     });
     low = group_reduce<THREADS>(other ? INFINITY : low, S.fpart, [](float a, float b) { return fmaxf(a, b); });
     constexpr int PER = VALUES / THREADS;
@@ -677,7 +683,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
     double border = -INFINITY;  // z - m of the least class that min-p keeps
     if (M32 > 0.f) border = (double)T32 * log((double)fminf(M32, 1.f));
     if constexpr (sizeof(T) == 2 && THREADS >= 512) {
-        if (T32 > 0.f && !(K > 0 && K < C)) {
+        // (short rows without top-p take as long either way: 1024 of 16,384 53 us by classes and 55 by values, of 32,768 79 and 74)
+        if (T32 > 0.f && !(K > 0 && K < C) && (P32 < 1.f || C > 16384)) {
             float m;
             uint64_t total = 0;
             const int j = draw_by_value(r, S, inv, P32, border, u, m, total);
