@@ -10,8 +10,8 @@
 // distance to it, and a list of all that is in the K-th's bin and above, on which the rest is done; for top-p without it an approximate
 // histogram of weights and one exact pass; otherwise one exact pass. An exact pass is bound by 64-bit arithmetic: 18 such instructions
 // and about as many others a class, 30 us for a row of 131,072 on a CU, where a reading takes 10. So long bf16 rows without top-k are
-// counted by value, in two passes (draw_by_value). 1024 rows of 131,072 bf16: the greatest 85 us, top-k 50 136, plain 155 (214 by classes),
-// top-p 0.9 159 (410); 37 rows of 50,021 bf16 28 and 34 (31 and 52). A row that has to be left to the other passes costs 7% more.
+// counted by value, in two passes (draw_by_value). 1024 rows of 131,072 bf16: the greatest 85 us, top-k 50 136, plain 131 (214 by classes),
+// top-p 0.9 135 (410); 37 rows of 50,021 bf16 26 and 32 (31 and 52). A row that has to be left to the other passes costs 7% more.
 #include <algorithm>
 #include <type_traits>
 
@@ -91,7 +91,7 @@ struct Shared {
             uint64_t lkey[LIST], skey[LIST];  // of listed classes key and place, one number in their common order
             uint64_t lw[LIST], sw[LIST];      // and weight
         };
-        uint64_t table[4 * LIST];  // weights by value (draw_by_value)
+        uint64_t table[4 * LIST + 2];  // weights by value (draw_by_value)
     };
     uint64_t found[2];
     unsigned listed, few;
@@ -525,25 +525,28 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
 
 // A bf16 of magnitude 2^-9 to 2^7 is one of 4096 values, and a long row has few of them, each many times. One pass counts them; weights,
 // the border of top-p and what min-p leaves are found from values and counts (with 4096 exponentials instead of one for every class), and
-// a second pass adds up a table's entries: 10 instructions a class and a reading of LDS instead of 36. Smaller magnitudes, one in a
-// thousand, are listed; a row with more of them, or with greater ones that matter, is left to the other passes.
+// a second pass adds up a table's entries: 8 instructions a class and a reading of LDS instead of 36. Smaller magnitudes, one in a
+// thousand, are listed; a row with more of them, or with greater ones that matter, is left to the other passes. Both passes treat a class like
+// any other and see to what is not counted once a vector or afterwards: 135 us for 1024 rows of 131,072, 157 with branches for each class.
 constexpr int VALUES = 4096, HALF = VALUES / 2, MAX_TINY = 1024;
 constexpr unsigned VALUES_FROM = 118u << 7;  // 2^-9
 
 __device__ __forceinline__ unsigned bits_of(const u32x4& v, int k) { return k & 1 ? v[k >> 1] >> 16 : v[k >> 1] & 0xFFFFu; }
-// (in falling order)
-__device__ __forceinline__ unsigned number_of(unsigned bits, unsigned above) { return bits >> 15 ? HALF + above : HALF - 1 - above; }
-__device__ __forceinline__ unsigned value_bits(int i) { return i < HALF ? VALUES_FROM + (HALF - 1 - i) : 0x8000u + VALUES_FROM + (i - HALF); }
+__device__ __forceinline__ unsigned above_of(const u32x4& v, int k) { return (bits_of(v, k) & 0x7FFFu) - VALUES_FROM; }
+__device__ __forceinline__ int number_of(const u32x4& v, int k, unsigned above) {  // in rising order; -1 and VALUES for above = HALF
+    return HALF + (int)(above ^ (unsigned)((int)(k & 1 ? v[k >> 1] : v[k >> 1] << 16) >> 31));
+}
+__device__ __forceinline__ unsigned value_bits(int i) { return i < HALF ? 0x8000u + VALUES_FROM + (HALF - 1 - i) : VALUES_FROM + (i - HALF); }
 __device__ __forceinline__ float bf16_value(unsigned bits) { return __uint_as_float(bits << 16); }
 
-// The sums of the values, those of small magnitude as one in the middle.
+// The sums of the values in falling order, those of small magnitude as one in the middle.
 struct ValueSums {
     const uint32_t* counts;
     const uint64_t* table;
     uint64_t tiny;
     __device__ __forceinline__ uint64_t operator[](int i) const {
         if (i == HALF) return tiny;
-        const int n = i - (i > HALF);
+        const int n = VALUES - 1 - i + (i > HALF);
         return counts[n] * table[n];
     }
 };
@@ -560,29 +563,37 @@ __device__ __forceinline__ int draw_by_value(const Row<T, THREADS, STAGED>& r, S
                                              float& m, uint64_t& total) {
     constexpr int VL = RowType<T>::VL, W = THREADS / 64, SEGMENTS = SAGE_MAX_CLASSES / (64 * U * VL);
     static_assert(VL == 8 && 64 * U * VL <= 1024 && Shared<THREADS>::BINS * 2 >= VALUES && Shared<THREADS>::LIST * 4 >= VALUES, "room in LDS");
-    static_assert(SEGMENTS + MAX_TINY / 2 <= Shared<THREADS>::SEGS, "room behind the segments");
+    static_assert(SEGMENTS + MAX_TINY <= Shared<THREADS>::SEGS, "room behind the segments");
     const int tid = r.tid;
     uint32_t* const counts = (uint32_t*)S.hist;
-    uint32_t* const tiny = (uint32_t*)(S.seg + SEGMENTS);
+    uint64_t* const tiny = S.seg + SEGMENTS;    // place and bits
+    uint64_t* const table = S.table + 1;        // (at its ends 0, for what is not counted)
     if (tid == 0) S.few = 0;
     clear_histogram(S, tid);
     float low = -INFINITY;  // greatest of the values below all counted ones
     bool other = false;     // NaN, or above all counted ones
-    r.template visit<true>([&](int, const u32x4* v) __attribute__((always_inline)) {
+    r.template visit<true>([&](int i, const u32x4* v) __attribute__((always_inline)) {
 #pragma unroll
         for (int q = 0; q < U; ++q) {
+            unsigned most = 0;
 #pragma unroll
             for (int k = 0; k < VL; ++k) {
                 if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                const unsigned h = bits_of(v[q], k), above = (h & 0x7FFFu) - VALUES_FROM;
-                if (above < (unsigned)HALF) {
-                    atomicAdd(&counts[number_of(h, above)], 1u);
-                } else if ((int)above >= 0) {
-                    if (h >> 15 && h <= 0xFF80u) low = fmaxf(low, bf16_value(h));
-                    else other = true;
-                } else {
-                    const unsigned p = atomicAdd(&S.few, 1u);
-                    if (p < (unsigned)MAX_TINY) tiny[p] = h;
+                const unsigned above = above_of(v[q], k);
+                if (above < (unsigned)HALF) atomicAdd(&counts[number_of(v[q], k, above)], 1u);
+                most = max(most, above);
+            }
+            if (most >= (unsigned)HALF) {
+#pragma unroll
+                for (int k = 0; k < VL; ++k) {
+                    const unsigned h = bits_of(v[q], k), above = above_of(v[q], k);
+                    if ((int)above < 0) {
+                        const unsigned p = atomicAdd(&S.few, 1u);
+                        if (p < (unsigned)MAX_TINY) tiny[p] = (uint64_t)(r.place(i, q) + k) << 16 | h;
+                    } else if (above >= (unsigned)HALF) {
+                        if (h >> 15 && h <= 0xFF80u) low = fmaxf(low, bf16_value(h));
+                        else other = true;
+                    }
                 }
             }
         }
@@ -590,44 +601,44 @@ __device__ __forceinline__ int draw_by_value(const Row<T, THREADS, STAGED>& r, S
     });
     low = group_reduce<THREADS>(other ? INFINITY : low, S.fpart, [](float a, float b) { return fmaxf(a, b); });
     constexpr int PER = VALUES / THREADS;
-    float first = VALUES;
+    float first = -1.f;
 #pragma unroll
-    for (int i = PER - 1; i >= 0; --i)
+    for (int i = 0; i < PER; ++i)
         if (counts[tid * PER + i]) first = (float)(tid * PER + i);
-    first = group_reduce<THREADS>(first, S.fpart + W, [](float a, float b) { return fminf(a, b); });
+    first = group_reduce<THREADS>(first, S.fpart + W, [](float a, float b) { return fmaxf(a, b); });
     const int few = (int)S.few;
-    if (low == INFINITY || first == (float)VALUES || few > (first < (float)HALF ? MAX_TINY : 0)) return -1;
+    if (low == INFINITY || first < 0.f || few > (first >= (float)HALF ? MAX_TINY : 0)) return -1;
     m = bf16_value(value_bits((int)first));
     const double md = m;
     if (((double)low - md) * inv > -29.9) return -1;  // (below -43 ln 2 there is no weight)
     auto weight = [&](float x) __attribute__((always_inline)) { return weight_of(((double)x - md) * inv); };
-    for (int i = tid; i < VALUES; i += THREADS) S.table[i] = counts[i] ? weight(bf16_value(value_bits(i))) : 0;
+    for (int i = tid; i < VALUES; i += THREADS) table[i] = counts[i] ? weight(bf16_value(value_bits(i))) : 0;
+    if (tid == 0) table[-1] = table[VALUES] = 0;
     uint64_t tiny_sum = 0;
-    for (int i = tid; i < few; i += THREADS) tiny_sum += weight(bf16_value(tiny[i]));
+    for (int i = tid; i < few; i += THREADS) tiny_sum += weight(bf16_value((unsigned)tiny[i] & 0xFFFFu));
     tiny_sum = group_sum<THREADS>(tiny_sum, S);  // (the table is there too)
-    int last = VALUES;         // the last value that top-p keeps any of
+    int last = -1;             // the last value that top-p keeps any of
     uint64_t kept = 0, at_last = 0;  // so many, if not all of it, of this weight
     if (P < 1.f) {
         uint64_t t = 0;
-        const int at = find_sum<THREADS>(S, ValueSums{counts, S.table, tiny_sum}, VALUES + 1, tid, total, [&](uint64_t all) {
+        const int at = find_sum<THREADS>(S, ValueSums{counts, table, tiny_sum}, VALUES + 1, tid, total, [&](uint64_t all) {
             const double q = ceil((double)P * (double)all);
             return t = q >= 1.0 ? (uint64_t)q - 1 : 0;
         });
         if (at == HALF) return -1;
-        last = at - (at > HALF);
-        at_last = S.table[last];
+        last = VALUES - 1 - at + (at > HALF);
+        at_last = table[last];
         kept = (t - S.found[0]) / at_last + 1;
         if (kept >= counts[last]) kept = 0;
     }
-    const float value = last < VALUES ? bf16_value(value_bits(last)) : -INFINITY;
+    const float value = last >= 0 ? bf16_value(value_bits(last)) : -INFINITY;
     __syncthreads();
     // what is left of the table; a value kept in part is counted
     for (int i = tid; i < VALUES; i += THREADS) {
-        if (i == last && kept) S.table[i] = 1ull << AT_BORDER;
-        else if (i > last || (double)bf16_value(value_bits(i)) - md < border) S.table[i] = 0;
+        if (i == last && kept) table[i] = 1ull << AT_BORDER;
+        else if (i < last || (double)bf16_value(value_bits(i)) - md < border) table[i] = 0;
     }
     if ((double)value - md < border) at_last = 0;
-    const bool tiny_kept = last >= HALF;
     auto drawn = [&](float x) __attribute__((always_inline)) { return weight(x) & mask_of((double)x - md >= border); };
     __syncthreads();
     r.visit([&](int i, const u32x4* v) __attribute__((always_inline)) {
@@ -637,15 +648,18 @@ __device__ __forceinline__ int draw_by_value(const Row<T, THREADS, STAGED>& r, S
 #pragma unroll
             for (int k = 0; k < VL; ++k) {
                 if (k % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                const unsigned h = bits_of(v[q], k), above = (h & 0x7FFFu) - VALUES_FROM;
-                if (above < (unsigned)HALF) own += S.table[number_of(h, above)];
-                else if (tiny_kept && (int)above < 0) own += drawn(bf16_value(h));
+                own += table[number_of(v[q], k, min(above_of(v[q], k), (unsigned)HALF))];
             }
         }
         const uint64_t s = wave_sum(own);
         if ((tid & 63) == 0) S.seg[i * W + (tid >> 6)] = s;
     });
     __syncthreads();
+    if (last < HALF) {
+        for (int i = tid; i < few; i += THREADS)
+            atomicAdd((unsigned long long*)&S.seg[r.segment_of((int)(tiny[i] >> 16))], (unsigned long long)drawn(bf16_value((unsigned)tiny[i] & 0xFFFFu)));
+        __syncthreads();
+    }
     Cut cut{value, 0x7FFFFFFF};
     if (kept) {
         const int seg = find_sum<THREADS>(S, BorderCounts{S.seg}, r.count * W, tid, total, [&](uint64_t) { return kept - 1; });
@@ -683,7 +697,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
     double border = -INFINITY;  // z - m of the least class that min-p keeps
     if (M32 > 0.f) border = (double)T32 * log((double)fminf(M32, 1.f));
     if constexpr (sizeof(T) == 2 && THREADS >= 512) {
-        // (short rows without top-p take as long either way: 1024 of 16,384 53 us by classes and 55 by values, of 32,768 79 and 74)
+        // (short rows without top-p take as long either way: 1024 of 16,384 53 us by classes and 54 by values, of 32,768 79 and 68)
         if (T32 > 0.f && !(K > 0 && K < C) && (P32 < 1.f || C > 16384)) {
             float m;
             uint64_t total = 0;
