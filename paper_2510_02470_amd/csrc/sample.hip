@@ -10,7 +10,7 @@
 // distance to it, and a list of all that is in the K-th's bin and above, on which the rest is done; for top-p without it an approximate
 // histogram of weights and one exact pass; otherwise one exact pass. An exact pass is bound by 64-bit arithmetic: 18 such instructions
 // and about as many others a class, 30 us for a row of 131,072 on a CU, where a reading takes 10. So long bf16 rows without top-k are
-// counted by value, in two passes (draw_by_value). 1024 rows of 131,072 bf16: the greatest 85 us, top-k 50 136, plain 131 (214 by classes),
+// counted by value, in two passes (draw_by_value). 1024 rows of 131,072 bf16: the greatest 85 us, top-k 50 136, plain 128 (214 by classes),
 // top-p 0.9 135 (410); 37 rows of 50,021 bf16 26 and 32 (31 and 52). A row that has to be left to the other passes costs 7% more.
 #include <algorithm>
 #include <type_traits>
