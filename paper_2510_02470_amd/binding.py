@@ -519,29 +519,30 @@ def logit_error(logits, labels, weights=None, out=None, dtype=None):
 MUON = (3.4445, -4.7750, 2.0315)  # of a step of orthogonalize: singular values end between about 0.7 and 1.2
 
 
-def _matrices(torch, G, dev, what):
-    """A matrix, or several, with rows or columns next to each other -> (batch, rows, cols, ld, stride, transposed)"""
-    _need(isinstance(G, torch.Tensor) and G.get_device() == dev and G.dim() in (2, 3) and G.shape[-2] >= 1 and G.shape[-1] >= 1, what)
-    rows, cols = G.shape[-2:]
-    batch = G.shape[0] if G.dim() == 3 else 1
-    sr, sc = G.stride(-2), G.stride(-1)
-    by_row = (cols == 1 or sc == 1) and (rows == 1 or sr >= cols)
-    by_col = (rows == 1 or sr == 1) and (cols == 1 or sc >= rows)
-    _need(by_row or by_col, what)
-    if not by_row:
-        rows, cols, sr, sc = cols, rows, sc, sr
-    ld = sr if rows > 1 else cols
-    stride = G.stride(0) if batch > 1 else (rows - 1) * ld + cols
-    _need(ld >= cols and stride >= (rows - 1) * ld + cols, what)
-    return batch, rows, cols, ld, stride, not by_row
+def _matrices(t, turned):
+    """A matrix, or several, as rows of elements next to each other, or (turned) its transpose as such: (batch, rows, cols, ld, stride), or
+    None if it does not lie in memory so. A single row or column can be either; elements further apart are only rows of one each."""
+    rows, cols = t.shape[-2:]
+    ld, step = t.stride()[-2:]
+    if turned:
+        rows, cols, ld, step = cols, rows, step, ld
+    if rows == 1:
+        ld = cols
+    batch = t.shape[0] if t.dim() == 3 else 1
+    one = (rows - 1) * ld + cols
+    stride = t.stride(0) if batch > 1 else one
+    if (cols > 1 and step != 1) or ld < cols or stride < one:
+        return None
+    return batch, rows, cols, ld, stride
 
 
 def orthogonalize(G, steps=5, coefficients=MUON, eps=1e-7, scale=1.0, out=None):
     """Matrices (rows x cols, or batch x rows x cols, float32 or bfloat16) made orthogonal by `steps` Newton-Schulz products: each step
     maps the singular values s to a s + b s^3 + c s^5, beginning with those of G / (||G||_F + eps); the result times scale.
 
-    G: rows or columns next to each other, at any stride (a transposed view too). coefficients: (a, b, c) for every step, or one
-    such triple for each. out: where the result goes, in the same order of rows and columns as G; possibly G itself.
+    G: rows or columns next to each other, at any stride (a transposed view too; of a single row or column the elements may be
+    apart). coefficients: (a, b, c) for every step, or one such triple for each. out: where the result goes, in the same order of
+    rows and columns as G; possibly G itself.
     """
     import torch
 
@@ -553,16 +554,23 @@ def orthogonalize(G, steps=5, coefficients=MUON, eps=1e-7, scale=1.0, out=None):
     _need(len(triples) == steps and all(len(t) == 3 for t in triples), what)
     flat = [float(v) for t in triples for v in t]
     dev = _device(torch, G, what)
-    batch, rows, cols, ld, stride, turned = _matrices(torch, G, dev, what)
+    _need(G.dim() in (2, 3) and G.shape[-2] >= 1 and G.shape[-1] >= 1, what)
     code = _code(torch, G.dtype, what)
+    if out is not None:
+        _need(isinstance(out, torch.Tensor) and out.get_device() == dev and out.dtype is G.dtype and out.shape == G.shape, what)
+    for turned in (False, True):  # the first way in which both can be described
+        layout = _matrices(G, turned)
+        out_layout = layout and out is not None and _matrices(out, turned)
+        if layout and (out is None or out_layout):
+            break
+    else:
+        _need(False, what)
+    batch, rows, cols, ld, stride = layout
     if out is None:
         out = torch.empty(G.shape[:-2] + (rows, cols), dtype=G.dtype, device="cuda")
         out = out.transpose(-1, -2) if turned else out
-    _need(isinstance(out, torch.Tensor) and out.dtype is G.dtype and out.shape == G.shape, what)
-    o_batch, o_rows, o_cols, o_ld, o_stride, o_turned = _matrices(torch, out, dev, what)
-    if o_turned != turned and 1 in (rows, cols):  # a single row or column may be called either
-        o_rows, o_cols, o_ld, o_turned = o_cols, o_rows, max(o_ld, o_cols), turned
-    _need(o_turned == turned, what)
+        out_layout = batch, rows, cols, cols, rows * cols
+    o_ld, o_stride = out_layout[3:]
     L = lib()
     need = C.c_size_t(0)
     _check(L.sage_orthogonalize_work(code, batch, rows, cols, C.byref(need)), what)

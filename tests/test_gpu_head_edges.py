@@ -1,0 +1,48 @@
+"""sample, logit_error and orthogonalize where layouts, settings and values meet that each alone are ordinary."""
+import math
+
+import numpy as np
+import pytest
+
+import head_reference as ref
+from test_gpu_head import MUON, _f32, _tdtype
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- orthogonalize ----------------------------------------------------------------------------------------------
+
+def _wide(t, step, fill):
+    """The same single row or column (or several), its elements `step` apart in memory that holds `fill`; and that memory."""
+    import torch
+
+    n, b = max(t.shape[-2:]), t.shape[0]
+    hold = torch.full((b, n * step + 3), fill, dtype=t.dtype, device="cuda")
+    view = hold[:, :n * step:step]
+    view = view[:, None, :] if t.shape[1] == 1 else view[:, :, None]
+    view.copy_(t)
+    return view, hold
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1, 100), (4, 1, 100), (4, 100, 1), (2, 1, 700)])
+def test_single_rows_whose_elements_are_apart(shape, dtype):
+    """What lies between the elements is not read, and left as it was."""
+    import torch
+    from paper_2510_02470_amd.binding import orthogonalize
+
+    g = torch.Generator(device="cuda").manual_seed(shape[-1])
+    G = torch.randn(shape, generator=g, device="cuda").to(_tdtype(dtype))
+    want = torch.stack([torch.from_numpy(ref.orthogonalize(x.double().cpu().numpy(), [[_f32(v) for v in MUON]] * 5, _f32(1e-7), 1.0)[0]) for x in G])
+    # a matrix of rank one: one singular value, of at most 1.25 after each step
+    tol = ref.orthogonalize_bound([1.0] * 5, [MUON] * 5, 1.0, G[0].numel()) + 1.01 * ref.HALF_STEP[dtype] * 1.25
+    for step, out_step in ((5, None), (5, 1), (1, 3), (2, 4), (1, 1)):
+        given, _ = _wide(G, step, math.nan)
+        out = hold = None
+        if out_step:
+            out, hold = _wide(torch.zeros_like(G), out_step, 7.0)
+        res = orthogonalize(given, out=out)
+        assert res.shape == G.shape and (out is None or res.data_ptr() == out.data_ptr())
+        assert float(torch.linalg.vector_norm(res.double().cpu() - want, dim=(1, 2)).max()) <= tol
+        if out_step:
+            assert int((hold == 7.0).sum()) == hold.numel() - G.numel()
