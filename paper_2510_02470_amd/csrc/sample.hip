@@ -216,6 +216,7 @@ __device__ __forceinline__ A wave_scan(A v, int lane) {  // sums up to and with 
     }
     return v;
 }
+// (Waves may still be reading S.part when others return: whoever writes it, this or find_sum, has them all meet first.)
 template <int THREADS>
 __device__ __forceinline__ uint64_t group_sum(uint64_t v, Shared<THREADS>& S) {
     v = wave_sum(v);
@@ -237,11 +238,13 @@ __device__ __forceinline__ uint64_t share_of(float u, uint64_t total) {
 }
 
 // The first of `count` sums (sums[i], of LDS) up to which they come to more than t = want(their total): its number, and in S.found the
-// sum of those before it and its own.
+// sum of those before it and its own. The work-group meets first: the sums may just have been written, and what this
+// writes may still be read.
 template <int THREADS, class E, class F>
 __device__ __forceinline__ int find_sum(Shared<THREADS>& S, E sums, int count, int tid, uint64_t& total, F want) {
     const int per = (count + THREADS - 1) / THREADS;
     uint64_t own = 0;
+    __syncthreads();
     for (int i = 0; i < per; ++i)
         if (tid * per + i < count) own += sums[tid * per + i];
     const uint64_t incl = wave_scan(own, tid & 63);
@@ -346,7 +349,6 @@ __device__ __forceinline__ int locate(const Row<T, THREADS, STAGED>& r, Shared<T
         const uint64_t s = wave_sum(own);
         if ((r.tid & 63) == 0) S.seg[i * W + (r.tid >> 6)] = s;
     });
-    __syncthreads();
     return locate_in(r, S, total, u, t0, [&](float x, int j) __attribute__((always_inline)) { return f(x, j) & mask_of(keeps(x, j)); });
 }
 
@@ -422,7 +424,6 @@ __device__ __forceinline__ Cut front(const Row<T, THREADS, STAGED>& r, Shared<TH
                 if (w) atomicAdd((unsigned long long*)&S.hist[b], (unsigned long long)w);
             }
         });
-        __syncthreads();
         uint64_t total;
         const int b = find_sum<THREADS>(S, (const uint64_t*)S.hist, S.BINS, r.tid, total, [&](uint64_t) { return t - above; });
         above += S.found[0];
@@ -495,7 +496,6 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
         clear_histogram(S, tid);
         for (int i = tid; i < count; i += THREADS)
             if (S.lkey[i] >= last) atomicAdd((unsigned long long*)&S.hist[bins(value(i))], (unsigned long long)S.lw[i]);
-        __syncthreads();
         uint64_t t = 0;
         const int at = find_sum<THREADS>(S, (const uint64_t*)S.hist, S.BINS, tid, total, [&](uint64_t all) {
             const double q = ceil((double)P * (double)all);
@@ -513,7 +513,6 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
     __syncthreads();
     for (int i = tid; i < count; i += THREADS)
         if (kept(i)) atomicAdd((unsigned long long*)&S.seg[r.segment_of(place(i))], (unsigned long long)S.lw[i]);
-    __syncthreads();
     const int seg = find_sum<THREADS>(S, (const uint64_t*)S.seg, r.count * r.W, tid, total, [&](uint64_t all) { return share_of(u, all); });
     const uint64_t base = S.found[0];
     return (int)~(uint32_t)passing(S, count, tid, base, share_of(u, total),
@@ -655,11 +654,9 @@ __device__ __forceinline__ int draw_by_value(const Row<T, THREADS, STAGED>& r, S
         if ((tid & 63) == 0) S.seg[i * W + (tid >> 6)] = s;
     });
     __syncthreads();
-    if (last < HALF) {
+    if (last < HALF)
         for (int i = tid; i < few; i += THREADS)
             atomicAdd((unsigned long long*)&S.seg[r.segment_of((int)(tiny[i] >> 16))], (unsigned long long)drawn(bf16_value((unsigned)tiny[i] & 0xFFFFu)));
-        __syncthreads();
-    }
     Cut cut{value, 0x7FFFFFFF};
     if (kept) {
         const int seg = find_sum<THREADS>(S, BorderCounts{S.seg}, r.count * W, tid, total, [&](uint64_t) { return kept - 1; });
@@ -669,7 +666,6 @@ __device__ __forceinline__ int draw_by_value(const Row<T, THREADS, STAGED>& r, S
             const uint64_t s = S.seg[i], n = i < seg ? s >> AT_BORDER : i == seg ? kept - before : 0;
             S.seg[i] = (s & ((1ull << AT_BORDER) - 1)) + n * at_last;
         }
-        __syncthreads();
     }
     return locate_in(r, S, total, &u, 0, [&](float x, int e) __attribute__((always_inline)) { return drawn(x) & mask_of(cut.keeps(x, e)); });
 }
@@ -746,7 +742,6 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
         r.each([&](float x, int) __attribute__((always_inline)) {
             if (x > -INFINITY) atomicAdd(&counts[kbins(x)], 1u);  // (masked classes, all in one bin, would wait for each other)
         });
-        __syncthreads();
         uint64_t all;
         const int b = find_sum<THREADS>(S, (const uint32_t*)counts, S.BINS, r.tid, all, [&](uint64_t) { return (uint64_t)K - 1; });
         const uint64_t before = S.found[0], through = before + S.found[1];
@@ -784,7 +779,6 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
             const uint32_t w = (uint32_t)__builtin_amdgcn_exp2f(fmaf(x - m, c2, 31.f));
             if (w) atomicAdd((unsigned long long*)&S.hist[bins(x)], (unsigned long long)w);
         });
-        __syncthreads();
         const int b = find_sum<THREADS>(S, (const uint64_t*)S.hist, S.BINS, r.tid, total, [&](uint64_t all) { return share_of(P32, all); });
         __syncthreads();
         if (r.tid == 0) S.listed = 0;

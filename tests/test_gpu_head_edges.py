@@ -46,3 +46,29 @@ def test_single_rows_whose_elements_are_apart(shape, dtype):
         assert float(torch.linalg.vector_norm(res.double().cpu() - want, dim=(1, 2)).max()) <= tol
         if out_step:
             assert int((hold == 7.0).sum()) == hold.numel() - G.numel()
+
+
+# ---- sample -----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("C", [33_001, 131_072])
+def test_long_rows_by_value_and_by_class_have_the_same_labels(C):
+    """bf16 rows, of whose values the weights are found by value, and the same rows as fp32, where every class is looked at: the border of
+    top-p moves with the sum of the values near zero, which work-groups add up on their own just before. All rows, again and again."""
+    import torch
+    from paper_2510_02470_amd.binding import sample
+
+    g = torch.Generator(device="cuda").manual_seed(C)
+    n = 600
+    z = 1.5 * torch.randn(n, C, generator=g, device="cuda") - 3.0
+    near = torch.randint(0, C, (n, 800), generator=g, device="cuda")
+    z.scatter_(1, near, 0.001 * torch.randn(n, 800, generator=g, device="cuda"))
+    z.scatter_(1, torch.randint(0, C, (n, 6), generator=g, device="cuda"), 2.0)
+    z = z.bfloat16()
+    wide = z.float()
+    u = torch.rand(n, generator=g, device="cuda")
+    p = torch.rand(n, generator=g, device="cuda")
+    for T in (1.0, 0.4):
+        want = sample(wide, u, temperature=T, top_p=p)
+        for _ in range(10):
+            labels, logp = sample(z, u, temperature=T, top_p=p)
+            assert torch.equal(labels, want[0]) and torch.equal(logp, want[1])
