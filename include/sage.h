@@ -337,7 +337,8 @@ int sage_topm_static(const float* alpha, int64_t N, int64_t m, int64_t* out_idx,
  *   top_k  > 0: the first top_k of them (0 or less, n_classes or more: all);
  *   top_p  < 1: with S the sum of the kept weights, the first, and every further one before which the kept weights sum to less than
  *               ceil(top_p * S) (NaN: all);
- *   min_p  > 0: those with z_j - max z >= temperature * ln(min(min_p, 1)).
+ *   min_p  > 0: those with z_j - max z >= temperature * ln(min_p); for a min_p of 1 or more those equal to the greatest, at any
+ *               temperature.
  * With S the sum of what is left and t = min(floor(u * S), S - 1) the label is the first class, by index, up to which the kept
  * weights sum to more than t. Equal rows and numbers give equal labels, whatever else is in the batch. A u below 0 (or NaN) counts
  * as 0, one of 1 or more takes the last kept class with a weight.

@@ -686,12 +686,13 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
 
     auto done = [&](int j, float m, double inv, uint64_t total) __attribute__((always_inline)) {
         if (r.tid != 0) return;
+        j = (int)min((unsigned)j, (unsigned)C - 1);  // (logits that change between the passes may leave no class: nothing is read behind the row)
         labels[row] = j;
         if (logp) logp[row] = (float)(((double)RowType<T>::widen(r.z[j]) - (double)m) * inv - log((double)total * 0x1p-42));
     };
     const double inv = 1.0 / (double)T32;
-    double border = -INFINITY;  // z - m of the least class that min-p keeps
-    if (M32 > 0.f) border = (double)T32 * log((double)fminf(M32, 1.f));
+    double border = -INFINITY;  // z - m of the least class that min-p keeps; never above 0: the greatest class stays
+    if (M32 > 0.f) border = M32 < 1.f ? (double)T32 * log((double)M32) : 0.0;  // (an infinite temperature times ln 1 is no number)
     if constexpr (sizeof(T) == 2 && THREADS >= 512) {
         // (short rows without top-p take as long either way: 1024 of 16,384 53 us by classes and 54 by values, of 32,768 79 and 68)
         if (T32 > 0.f && !(K > 0 && K < C) && (P32 < 1.f || C > 16384)) {

@@ -72,3 +72,46 @@ def test_long_rows_by_value_and_by_class_have_the_same_labels(C):
         for _ in range(10):
             labels, logp = sample(z, u, temperature=T, top_p=p)
             assert torch.equal(labels, want[0]) and torch.equal(logp, want[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,C", [(6, 1), (6, 5), (8, 700), (8, 9001), (8, 40_000), (260, 33_001)])
+def test_min_p_of_one_at_any_temperature(n, C, dtype):
+    """What is left are the classes equal to the greatest, of those that the other settings leave; at an infinite temperature too,
+    where all classes that are not masked have the same weight."""
+    import torch
+    from paper_2510_02470_amd.binding import sample
+
+    rng = np.random.default_rng(C)
+    z = 2.0 * rng.standard_normal((n, C))
+    z[rng.random(z.shape) < 0.3] = -np.inf
+    z[:, C // 2] = 1.0
+    z[1] = np.round(z[1])  # several greatest
+    z[2] = 0.25
+    z[3] = np.where(np.arange(C) % 3 == 1, 9.0, z[3])
+    z[4] = -np.inf
+    z[4, C - 1] = -5.0
+    zd = torch.from_numpy(z).cuda().to(_tdtype(dtype))
+    zh = zd.double().cpu().numpy()
+    u = rng.random(n, dtype=np.float32)
+    ud = torch.from_numpy(u).cuda()
+    for T in (math.inf, 1.0, 1e30):
+        for k, p in ((0, 1.0), (3, 1.0), (0, 0.6), (3, 0.5), (max(1, 2 * C // 3), 0.9)):
+            for m in (1.0, 2.0, math.inf):
+                labels, logp = (t.cpu().numpy() for t in sample(zd, ud, temperature=T, top_k=k, top_p=p, min_p=m))
+                for i in range(n if n < 100 else 12):
+                    kept, w = ref.kept_classes(zh[i], T, k, _f32(p), 0.0)
+                    kept = kept[zh[i, kept] == zh[i].max()]
+                    c = np.cumsum(w[kept])
+                    j = kept[np.searchsorted(c, min(int(float(u[i]) * float(c[-1])), int(c[-1]) - 1), side="right")]
+                    assert labels[i] == j, (T, k, p, m, i, labels[i], j)
+                    assert abs(logp[i] + math.log(len(kept))) <= 2.0 ** -24 * math.log(len(kept)) + 1e-12
+    # as one request among others
+    per_row = lambda values: torch.from_numpy(np.resize(np.float32(values), n)).cuda()
+    T, m = np.resize(np.float32([math.inf, 1.0, math.inf, 0.7]), n), np.resize(np.float32([1.0, 0.1, 0.1]), n)
+    labels, _ = sample(zd, ud, temperature=per_row([math.inf, 1.0, math.inf, 0.7]), min_p=per_row([1.0, 0.1, 0.1]))
+    for i, j in enumerate(labels.cpu().numpy()):
+        if T[i] < math.inf or m[i] < 1:
+            assert j == ref.sample_row(zh[i], float(u[i]), float(T[i]), 0, 1.0, float(m[i]))[0]
+        else:
+            assert zh[i, j] == zh[i].max()
