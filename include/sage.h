@@ -371,9 +371,10 @@ int sage_sample(const void* logits, sage_dtype dtype, int64_t rows, int64_t n_cl
  * E are NaN. weights: DEVICE, one fp32 per row (the gradient of whatever is made of the losses), or NULL: 1. E: DEVICE, row i
  * starts at element i * ld_e, of type e_dtype; may be the logits' own memory if type and ld are theirs, and must not overlap it
  * otherwise (SAGE_ERR_ARG); or NULL. loss: DEVICE, one fp32 per row, or NULL. Columns behind the classes are neither read nor
- * written. Sums are fp32; E_iy is formed from the other classes' sum, so that it keeps its digits where the label's probability
- * is nearly 1. Logits of -inf have probability 0; a label among them has an infinite loss; a row of nothing else has an infinite loss
- * and E zero. A NaN or +inf in a row with a label makes its loss and E NaN. Asynchronous on hip_stream; allocates nothing.
+ * written. Sums are fp32, of exponentials good to fp32 whatever e_dtype is; E_iy is formed from the other classes' sum, so that it
+ * keeps its digits where the label's probability is nearly 1. Logits of -inf have probability 0; a label among them has an infinite
+ * loss; a row of nothing else has an infinite loss and E zero. A NaN or +inf in a row with a label makes its loss and E NaN.
+ * Asynchronous on hip_stream; allocates nothing.
  */
 int sage_logit_error(const void* logits, sage_dtype dtype, int64_t rows, int64_t n_classes, int64_t ld, const int32_t* labels,
                      const float* weights, void* E, sage_dtype e_dtype, int64_t ld_e, float* loss, void* hip_stream);

@@ -16,8 +16,8 @@
 namespace sage {
 namespace {
 
-// e^(x - m): the difference is exact or rounded once; the product with log2 e is carried to twice the width where WIDE (a bf16 result
-// does not show the 2^-20 that a difference of 16 loses otherwise).
+// e^(x - m): the difference is exact or rounded once; the product with log2 e is carried to twice the width where WIDE. Without it a
+// difference of 16 loses 2^-20, which a bf16 E does not show; the sums always have it, for the loss is fp32 whatever E is.
 template <bool WIDE>
 __device__ __forceinline__ float exp_diff(float x, float m) {
     const float d = x - m;
@@ -106,7 +106,6 @@ __global__ __launch_bounds__(THREADS * ROWS) void logit_error_kernel(ErrorArgs<T
     static_assert(ROWS == 1 || THREADS == 64, "a row of several waves has the work-group's barrier");
     __shared__ float2 wave_part[THREADS / 64];
     constexpr int VL = RowType<T>::VL;
-    constexpr bool WIDE = sizeof(TE) == 4;
     // a row's work-groups each read all of it and write a part
     const int parts = N == 0 ? a.parts : 1, part = N == 0 ? blockIdx.x % a.parts : 0;
     const int64_t row = N == 0 ? blockIdx.x / a.parts : (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
@@ -186,9 +185,9 @@ __global__ __launch_bounds__(THREADS * ROWS) void logit_error_kernel(ErrorArgs<T
         float top = m;
 #pragma unroll
         for (int i = 0; i < VL; ++i) top = fmaxf(top, RowType<T>::at(v, i));
-        float sum = rest * exp_diff<WIDE>(m, top);
+        float sum = rest * exp_diff<true>(m, top);
 #pragma unroll
-        for (int i = 0; i < VL; ++i) sum += exp_diff<WIDE>(RowType<T>::at(v, i), top);
+        for (int i = 0; i < VL; ++i) sum += exp_diff<true>(RowType<T>::at(v, i), top);
         m = top;
         rest = sum;
     });
@@ -196,7 +195,7 @@ __global__ __launch_bounds__(THREADS * ROWS) void logit_error_kernel(ErrorArgs<T
     float top = m;
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    rest *= exp_diff<WIDE>(m, top);
+    rest *= exp_diff<true>(m, top);
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) rest += __shfl_xor(rest, d, 64);
     m = top;
@@ -210,7 +209,7 @@ __global__ __launch_bounds__(THREADS * ROWS) void logit_error_kernel(ErrorArgs<T
         for (int i = 0; i < THREADS / 64; ++i) m = fmaxf(m, w[i].x);
         rest = 0.f;
 #pragma unroll
-        for (int i = 0; i < THREADS / 64; ++i) rest += w[i].y * exp_diff<WIDE>(w[i].x, m);
+        for (int i = 0; i < THREADS / 64; ++i) rest += w[i].y * exp_diff<true>(w[i].x, m);
     }
     const float ey = exp_diff<true>(zy, m), S = rest + ey;
     if (a.loss && tid == 0 && part == 0) a.loss[row] = row_loss(rest, ey, zy, m);

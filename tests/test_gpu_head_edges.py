@@ -115,3 +115,47 @@ def test_min_p_of_one_at_any_temperature(n, C, dtype):
             assert j == ref.sample_row(zh[i], float(u[i]), float(T[i]), 0, 1.0, float(m[i]))[0]
         else:
             assert zh[i, j] == zh[i].max()
+
+
+# ---- logit_error ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,C", [(3000, 2), (40, 1000), (5, 9001), (300, 40_000), (3, 140_001), (260, 90_001)])
+def test_losses_do_not_depend_on_the_type_of_the_errors(n, C, dtype):
+    import ctypes
+
+    import torch
+    from paper_2510_02470_amd import binding
+
+    g = torch.Generator(device="cuda").manual_seed(C)
+    z = (3 * torch.randn(n, C, generator=g, device="cuda")).to(_tdtype(dtype))
+    y = torch.randint(0, C, (n,), generator=g, device="cuda", dtype=torch.int32)
+    y = torch.where(torch.arange(n, device="cuda") % 2 == 0, z.float().argmax(1).int(), y)
+    wide = binding.logit_error(z, y, dtype=torch.float32)[1]
+    narrow = binding.logit_error(z, y, dtype=torch.bfloat16)[1]
+    assert torch.equal(wide, narrow)
+    alone = torch.zeros_like(wide)
+    p = lambda t: ctypes.c_void_p(t.data_ptr())
+    code = binding.SAGE_BF16 if dtype == "bf16" else binding.SAGE_F32
+    for e_code in (binding.SAGE_F32, binding.SAGE_BF16):
+        rc = binding.lib().sage_logit_error(p(z), code, n, C, C, p(y), None, None, e_code, C, p(alone), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert rc == binding.SAGE_OK and torch.equal(alone, wide)
+        alone.zero_()
+
+
+def test_losses_of_learnt_examples_with_one_rival():
+    """log1p(e^-d): d is exact, the exponential is off by an ulp (2^-23) of the power of two and half of one (2^-24) of what is added to it for
+    the rest of the product d log2 e, and the loss is rounded once (2^-24): four half steps, and one for the products of these."""
+    import torch
+    from paper_2510_02470_amd.binding import logit_error
+
+    for shift in (0.0, 3.0, -40.0):
+        z = torch.zeros(4000, 2, device="cuda", dtype=torch.bfloat16)
+        z[:, 0] = shift
+        z[:, 1] = shift - torch.linspace(0.05, 80.0, 4000, device="cuda")
+        d = (z[:, 0].double() - z[:, 1].double())
+        want = torch.log1p(torch.exp(-d))
+        for dtype in (torch.bfloat16, torch.float32):
+            _, loss = logit_error(z, torch.zeros(4000, device="cuda", dtype=torch.int32), dtype=dtype)
+            err = (loss.double() - want).abs() / want
+            assert float(err.max()) <= 5 * 2.0 ** -24, (dtype, shift, float(err.max()))
