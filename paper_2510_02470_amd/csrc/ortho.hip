@@ -846,9 +846,10 @@ double bound_of(double a, double b, double c, double top, bool odd) {
     double root[2] = {-1.0, -1.0};
     if (A != 0.0) {
         const double d = B * B - 4 * A * C;
-        if (d >= 0.0) {
-            root[0] = (-B + sqrt(d)) / (2 * A);
-            root[1] = (-B - sqrt(d)) / (2 * A);
+        if (d >= 0.0) {  // (the root that is a difference of nearly equal numbers, where A is small, is C over the other's numerator)
+            const double q = -0.5 * (B + copysign(sqrt(d), B));
+            root[0] = q / A;
+            if (q != 0.0) root[1] = C / q;
         }
     } else if (B != 0.0) {
         root[0] = -C / B;

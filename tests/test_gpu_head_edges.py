@@ -159,3 +159,26 @@ def test_losses_of_learnt_examples_with_one_rival():
             _, loss = logit_error(z, torch.zeros(4000, device="cuda", dtype=torch.int32), dtype=dtype)
             err = (loss.double() - want).abs() / want
             assert float(err.max()) <= 5 * 2.0 ** -24, (dtype, shift, float(err.max()))
+
+
+# ---- orthogonalize: coefficients --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("m,n", [(24, 40), (150, 140)])
+def test_nearly_cubic_coefficients(m, n):
+    """Singular values stretched past the extreme of the next step's polynomial, whose fifth power is as good as none."""
+    import torch
+    from paper_2510_02470_amd.binding import orthogonalize
+
+    g = torch.Generator(device="cuda").manual_seed(m)
+    Q = torch.linalg.qr(torch.randn(m, m, generator=g, device="cuda", dtype=torch.float64).cpu())[0]
+    G = torch.zeros(m, n, dtype=torch.float64)
+    k = min(m, n, 20)
+    G[:, :k] = Q[:, :k] * torch.linspace(0.05, 1.0, k, dtype=torch.float64)
+    G = G.float()
+    # the bound of the first step's singular values is 1.732, where 1.5 s - 0.5 s^3 is next to 0; at 1 it is 1
+    triples = [(1.7287, 0.0, 0.0), (1.5, -0.5, 1e-30), (1.5, -0.5, -1e-25)]
+    out = orthogonalize(G.cuda(), steps=3, coefficients=triples, eps=0.0).double().cpu().numpy()
+    want, norms = ref.orthogonalize(G.double().numpy(), [[_f32(v) for v in t] for t in triples], 0.0, 1.0)
+    # singular values up to 1.73: slopes up to 3, the terms' sum at most 1.5 * 1.73 + 0.5 * 1.73^3 = 5.2
+    tol = ref.orthogonalize_bound(norms, [(3.0, -1.1, 0.0)] * 3, 1.0, m * n)
+    assert np.linalg.norm(out - want) <= tol
