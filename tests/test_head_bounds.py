@@ -37,3 +37,10 @@ def test_bounds_are_those_of_a_grid():
         # (2^-10 is added to the bound after every step)
         assert _rc((a, b, c), (f * (1 - 2.0 ** -8), 0.0, 0.0)) == SAGE_OK, (a, b, c)
         assert _rc((a, b, c), (f * (1 + 2.0 ** -12), 0.0, 0.0)) == SAGE_ERR_ARG, (a, b, c)
+
+
+def test_coefficients_of_up_to_1024_are_taken():
+    """Greater ones are not, also where what they make of singular values stays below 2^10."""
+    assert _rc((1024.0, -1024.0, 0.0)) == SAGE_OK and _rc((-1024.0, 1024.0, 0.0)) == SAGE_OK and _rc((0.0, 1000.0, -1024.0)) == SAGE_OK
+    for t in ((1025.0, -1025.0, 0.0), (2000.0, -2000.0, 0.0), (0.0, -1025.0, 1024.0), (0.0, 1024.0, -1025.0)):
+        assert _rc(t) == SAGE_ERR_ARG
