@@ -323,7 +323,7 @@ __device__ __forceinline__ int locate_in(const Row<T, THREADS, STAGED>& r, Share
     return locate_at(r, S, seg, S.found[0], u ? share_of(*u, total) : t0, f);
 }
 
-// The same from the row alone. keeps(value, element): f is not 0; bits(value, element): f, and ROUND_BITS if `rounded`, for what is kept.
+// The same from the row alone. keeps(value, element): whether it counts at all; f(value, element): what it counts if so, a whole number.
 template <class T, int THREADS, bool STAGED, class K, class F>
 __device__ __forceinline__ int locate(const Row<T, THREADS, STAGED>& r, Shared<THREADS>& S, uint64_t& total, const float* u, uint64_t t0, K keeps, F f) {
     constexpr int VL = RowType<T>::VL, W = THREADS / 64;
