@@ -370,11 +370,11 @@ int sage_sample(const void* logits, sage_dtype dtype, int64_t rows, int64_t n_cl
  * logits as for sage_sample. labels: DEVICE, one int32 y per row; a row with y < 0 has none: loss 0, E zero. y >= n_classes: loss and
  * E are NaN. weights: DEVICE, one fp32 per row (the gradient of whatever is made of the losses), or NULL: 1. E: DEVICE, row i
  * starts at element i * ld_e, of type e_dtype; may be the logits' own memory if type and ld are theirs, and must not overlap it
- * otherwise (SAGE_ERR_ARG); or NULL. loss: DEVICE, one fp32 per row, or NULL. Columns behind the classes are neither read nor
- * written. Sums are fp32, of exponentials good to fp32 whatever e_dtype is; E_iy is formed from the other classes' sum, so that it
- * keeps its digits where the label's probability is nearly 1. Logits of -inf have probability 0; a label among them has an infinite
- * loss; a row of nothing else has an infinite loss and E zero. A NaN or +inf in a row with a label makes its loss and E NaN.
- * Asynchronous on hip_stream; allocates nothing.
+ * otherwise (SAGE_ERR_ARG; rows that are as many bytes apart may lie between the logits' rows); or NULL. loss: DEVICE, one fp32 per
+ * row, or NULL. Columns behind the classes are neither read nor written. Sums are fp32, of exponentials good to fp32 whatever e_dtype
+ * is; E_iy is formed from the other classes' sum, so that it keeps its digits where the label's probability is nearly 1. Logits of -inf
+ * have probability 0; a label among them has an infinite loss; a row of nothing else has an infinite loss and E zero. A NaN or +inf
+ * in a row with a label makes its loss and E NaN. Asynchronous on hip_stream; allocates nothing.
  */
 int sage_logit_error(const void* logits, sage_dtype dtype, int64_t rows, int64_t n_classes, int64_t ld, const int32_t* labels,
                      const float* weights, void* E, sage_dtype e_dtype, int64_t ld_e, float* loss, void* hip_stream);
@@ -384,10 +384,10 @@ int sage_logit_error(const void* logits, sage_dtype dtype, int64_t rows, int64_t
  *     X = G / (||G||_F + eps);   then, for each of the steps, with A = X X^T:   X <- a X + (b A + c A A) X;   out = scale * X.
  * Each step maps the singular values s of X to a s + b s^3 + c s^5 and leaves its singular vectors. G: DEVICE, `batch` matrices of
  * rows x cols, element (i, r, t) at i * stride + r * ld + t; out: DEVICE, of the same type, with stride_out and ld_out; the two
- * must not overlap unless they are the same memory with the same strides. coefficients: HOST, 3 * steps floats (a, b, c of each
- * step), none beyond 2^10 in magnitude. batch >= 0, 1 <= rows, cols <= 32768, 1 <= steps <= 32, eps >= 0, ld >= cols, batched
- * matrices disjoint. SAGE_ERR_ARG also for coefficients under which singular values in [0, 1] pass 2^10 on the way. A zero matrix
- * gives zero.
+ * must not overlap unless they are the same memory with the same strides (with the same strides the rows of one may lie between
+ * those of the other). coefficients: HOST, 3 * steps floats (a, b, c of each step), none beyond 2^10 in magnitude. batch >= 0,
+ * 1 <= rows, cols <= 32768, 1 <= steps <= 32, eps >= 0, ld >= cols, batched matrices disjoint. SAGE_ERR_ARG also for
+ * coefficients under which singular values in [0, 1] pass 2^10 on the way. A zero matrix gives zero.
  * X, A and the polynomial are kept as two fp16 parts, scaled by the bound U of the singular values that the coefficients give (1 before the
  * first step): 22 bits and more of entries above 2^-17 U, 2^-39 U of smaller ones. Products of parts are summed in fp32, the norm in
  * fp64. So the result is good to fp32 rounding of the products, for both types, unless eps is so large beside the norm that X

@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "logit_rows.h"
+#include "rows_meet.h"
 #include "sage_internal.h"
 
 namespace sage {
@@ -1071,7 +1072,10 @@ extern "C" int sage_orthogonalize(const void* G, sage_dtype dtype, int64_t batch
         const uintptr_t g0 = (uintptr_t)G, o0 = (uintptr_t)out;
         const uintptr_t g1 = g0 + es * ((batch > 1 ? (batch - 1) * stride : 0) + (rows - 1) * ld + cols);
         const uintptr_t o1 = o0 + es * ((batch > 1 ? (batch - 1) * stride_out : 0) + (rows - 1) * ld_out + cols);
-        if (g0 < o1 && o0 < g1) return SAGE_ERR_ARG;
+        const bool alike = (rows == 1 || ld == ld_out) && (batch == 1 || stride == stride_out);  // (else they are taken to meet where their spans do)
+        const int64_t apart = batch > 1 ? stride : (rows - 1) * ld + cols;
+        if (g0 < o1 && o0 < g1 && !(alike && !groups_meet((int64_t)(o0 - g0), es * apart, batch, es * ld, rows, es * cols, es * cols)))
+            return SAGE_ERR_ARG;
     }
     const Plan p = plan_of(batch, rows, cols);
     if (!work || (uintptr_t)work % 256 || work_bytes < (size_t)p.bytes) return SAGE_ERR_ARG;

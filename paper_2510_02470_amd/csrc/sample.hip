@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "logit_rows.h"
+#include "rows_meet.h"
 #include "sage_internal.h"
 #include "wave_ops.h"
 
@@ -893,9 +894,11 @@ bool logit_rows_ok(const void* p, int dtype, int64_t rows, int64_t C, int64_t ld
 bool rows_overlap(const void* a, int da, int64_t lda, const void* b, int db, int64_t ldb, int64_t rows, int64_t C) {
     if (rows == 0) return false;
     const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-    const uintptr_t a1 = a0 + ((uint64_t)(rows - 1) * lda + C) * (da == SAGE_BF16 ? 2 : 4);
-    const uintptr_t b1 = b0 + ((uint64_t)(rows - 1) * ldb + C) * (db == SAGE_BF16 ? 2 : 4);
-    return a0 < b1 && b0 < a1;
+    const int64_t ea = da == SAGE_BF16 ? 2 : 4, eb = db == SAGE_BF16 ? 2 : 4;
+    const uintptr_t a1 = a0 + ((rows - 1) * lda + C) * ea, b1 = b0 + ((rows - 1) * ldb + C) * eb;
+    if (a0 >= b1 || b0 >= a1) return false;
+    // (rows of other distances are taken to meet where their spans do)
+    return rows == 1 || lda * ea != ldb * eb || rows_meet((int64_t)(b0 - a0), lda * ea, rows, C * ea, C * eb);
 }
 
 }  // namespace sage

@@ -182,3 +182,56 @@ def test_nearly_cubic_coefficients(m, n):
     # singular values up to 1.73: slopes up to 3, the terms' sum at most 1.5 * 1.73 + 0.5 * 1.73^3 = 5.2
     tol = ref.orthogonalize_bound(norms, [(3.0, -1.1, 0.0)] * 3, 1.0, m * n)
     assert np.linalg.norm(out - want) <= tol
+
+
+# ---- outputs between the rows of the inputs ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,C", [(1, 9), (5, 40), (300, 1001), (4, 70_001), (2, 140_000)])
+def test_errors_beside_their_logits(n, C, dtype):
+    """Columns of one buffer: what is before, between and behind them stays as it was."""
+    import torch
+    from paper_2510_02470_amd.binding import SageError, logit_error
+
+    g = torch.Generator(device="cuda").manual_seed(C)
+    z = (3 * torch.randn(n, C, generator=g, device="cuda")).to(_tdtype(dtype))
+    y = torch.randint(0, C, (n,), generator=g, device="cuda", dtype=torch.int32)
+    want, want_loss = logit_error(z, y)
+    for first, second in ((3, C + 3), (C + 9, 4)):
+        buf = torch.full((n, 2 * C + 20), 7.0, dtype=z.dtype, device="cuda")
+        logits, E = buf[:, first:first + C], buf[:, second:second + C]
+        logits.copy_(z)
+        loss = logit_error(logits, y, out=E)[1]
+        assert torch.equal(E, want) and torch.equal(loss, want_loss) and torch.equal(logits, z)
+        E.fill_(7.0)
+        logits.fill_(7.0)
+        assert bool((buf == 7.0).all())
+        for shift in (-1, 1, C - 1, 1 - C):
+            if n > 1 and 0 <= first + shift:
+                with pytest.raises(SageError):
+                    logit_error(logits, y, out=buf[:, first + shift:first + shift + C])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,m,n", [(1, 5, 9), (3, 130, 70), (2, 64, 200), (1, 1, 30)])
+def test_updates_beside_their_gradients(b, m, n, dtype):
+    import torch
+    from paper_2510_02470_amd.binding import SageError, orthogonalize
+
+    g = torch.Generator(device="cuda").manual_seed(n)
+    G = torch.randn(b, m, n, generator=g, device="cuda").to(_tdtype(dtype))
+    want = orthogonalize(G)
+    for first, second in ((2, n + 2), (n + 7, 3)):
+        buf = torch.full((b, m + 1, 2 * n + 10), 7.0, dtype=G.dtype, device="cuda")
+        given, out = buf[:, :m, first:first + n], buf[:, :m, second:second + n]
+        given.copy_(G)
+        orthogonalize(given, out=out)
+        assert torch.equal(out, want) and torch.equal(given, G)
+        out.fill_(7.0)
+        given.fill_(7.0)
+        assert bool((buf == 7.0).all())
+        with pytest.raises(SageError):
+            orthogonalize(given, out=buf[:, :m, first + 1:first + 1 + n])
+        if m > 1:
+            with pytest.raises(SageError):
+                orthogonalize(given, out=buf[:, 1:, first:first + n])

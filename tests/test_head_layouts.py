@@ -1,5 +1,8 @@
 """Where sage_orthogonalize is told to read and write for matrices of every layout: the calls are recorded and compared with the
 tensors' own addresses. No GPU."""
+import os
+import subprocess
+
 import numpy as np
 import pytest
 import torch
@@ -98,3 +101,16 @@ def test_refused_layouts(recorder):
                    (torch.zeros(1, 9), torch.zeros(1, 1).expand(1, 9))):
         with pytest.raises(binding.SageError):
             binding.orthogonalize(G, out=out)
+
+
+def test_common_elements_of_rows(tmp_path):
+    """rows_meet_check.cc; and the check itself: it must refuse a comparison of the spans."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    exe = str(tmp_path / "rows_meet_check")
+    csrc = os.path.join(os.path.dirname(here), "paper_2510_02470_amd", "csrc")
+    b = subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Werror", "-I", csrc, os.path.join(here, "rows_meet_check.cc"), "-o", exe],
+                       capture_output=True, text=True)
+    assert b.returncode == 0, b.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "rows_meet_check ok" in r.stdout, r.stdout
+    assert subprocess.run([exe, "spans"], capture_output=True, text=True, timeout=120).returncode == 1
