@@ -386,8 +386,9 @@ int sage_logit_error(const void* logits, sage_dtype dtype, int64_t rows, int64_t
  * rows x cols, element (i, r, t) at i * stride + r * ld + t; out: DEVICE, of the same type, with stride_out and ld_out; the two
  * must not overlap unless they are the same memory with the same strides (with the same strides the rows of one may lie between
  * those of the other). coefficients: HOST, 3 * steps floats (a, b, c of each step), none beyond 2^10 in magnitude. batch >= 0,
- * 1 <= rows, cols <= 32768, 1 <= steps <= 32, eps >= 0, ld >= cols, batched matrices disjoint. SAGE_ERR_ARG also for
- * coefficients under which singular values in [0, 1] pass 2^10 on the way. A zero matrix gives zero.
+ * 1 <= rows, cols <= 32768, 1 <= steps <= 32, eps >= 0, ld >= cols, batched matrices behind each other (stride >= (rows - 1) *
+ * ld + cols) or side by side (stride >= cols, (batch - 1) * stride + cols <= ld). SAGE_ERR_ARG also for coefficients under which
+ * singular values in [0, 1] pass 2^10 on the way. A zero matrix gives zero.
  * X, A and the polynomial are kept as two fp16 parts, scaled by the bound U of the singular values that the coefficients give (1 before the
  * first step): 22 bits and more of entries above 2^-17 U, 2^-39 U of smaller ones. Products of parts are summed in fp32, the norm in
  * fp64. So the result is good to fp32 rounding of the products, for both types, unless eps is so large beside the norm that X

@@ -531,7 +531,8 @@ def _matrices(t, turned):
     batch = t.shape[0] if t.dim() == 3 else 1
     one = (rows - 1) * ld + cols
     stride = t.stride(0) if batch > 1 else one
-    if (cols > 1 and step != 1) or ld < cols or stride < one:
+    side_by_side = rows > 1 and stride >= cols and (batch - 1) * stride + cols <= ld  # the column slices of one matrix
+    if (cols > 1 and step != 1) or ld < cols or not (stride >= one or side_by_side):
         return None
     return batch, rows, cols, ld, stride
 
@@ -540,8 +541,8 @@ def orthogonalize(G, steps=5, coefficients=MUON, eps=1e-7, scale=1.0, out=None):
     """Matrices (rows x cols, or batch x rows x cols, float32 or bfloat16) made orthogonal by `steps` Newton-Schulz products: each step
     maps the singular values s to a s + b s^3 + c s^5, beginning with those of G / (||G||_F + eps); the result times scale.
 
-    G: rows or columns next to each other, at any stride (a transposed view too; of a single row or column the elements may be
-    apart). coefficients: (a, b, c) for every step, or one such triple for each. out: where the result goes, in the same order of
+    G: rows or columns next to each other, at any stride (a transposed view too, or the column slices of one matrix as a batch; of a
+    single row or column the elements may be apart). coefficients: (a, b, c) for every step, or one such triple for each. out: where the result goes, in the same order of
     rows and columns as G; possibly G itself.
     """
     import torch

@@ -1033,11 +1033,16 @@ bool sizes_ok(int dtype, int64_t batch, int64_t rows, int64_t cols) {
            cols <= MAX_SIDE;
 }
 
-// rows of `cols` every ld, matrices every stride, none reaching into another, all offsets in 62 bits
+// matrices whose rows are side by side in rows of ld (the column slices of one matrix); else one is behind the other
+bool side_by_side(int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride) {
+    return batch > 1 && rows > 1 && stride >= cols && stride <= ld / (batch - 1) && (batch - 1) * stride + cols <= ld;
+}
+
+// rows of `cols` every ld, matrices every stride, none with an element of another, all offsets in 62 bits
 bool layout_ok(const void* p, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride) {
     if (!p || (uintptr_t)p % (dtype == SAGE_BF16 ? 2 : 4) || ld < cols || ld > (1ll << 40)) return false;
     const int64_t one = (rows - 1) * ld + cols;
-    return batch <= 1 || (stride >= one && stride <= (1ll << 59) / batch);
+    return batch <= 1 || side_by_side(batch, rows, cols, ld, stride) || (stride >= one && stride <= (1ll << 59) / batch);
 }
 
 }  // namespace
@@ -1073,8 +1078,10 @@ extern "C" int sage_orthogonalize(const void* G, sage_dtype dtype, int64_t batch
         const uintptr_t g1 = g0 + es * ((batch > 1 ? (batch - 1) * stride : 0) + (rows - 1) * ld + cols);
         const uintptr_t o1 = o0 + es * ((batch > 1 ? (batch - 1) * stride_out : 0) + (rows - 1) * ld_out + cols);
         const bool alike = (rows == 1 || ld == ld_out) && (batch == 1 || stride == stride_out);  // (else they are taken to meet where their spans do)
-        const int64_t apart = batch > 1 ? stride : (rows - 1) * ld + cols;
-        if (g0 < o1 && o0 < g1 && !(alike && !groups_meet((int64_t)(o0 - g0), es * apart, batch, es * ld, rows, es * cols, es * cols)))
+        const int64_t d = (int64_t)(o0 - g0), apart = es * (batch > 1 ? stride : (rows - 1) * ld + cols), pitch = es * ld, width = es * cols;
+        if (g0 < o1 && o0 < g1 &&
+            (!alike || (side_by_side(batch, rows, cols, ld, stride) ? groups_meet(d, pitch, rows, apart, batch, width, width)
+                                                                    : groups_meet(d, apart, batch, pitch, rows, width, width))))
             return SAGE_ERR_ARG;
     }
     const Plan p = plan_of(batch, rows, cols);

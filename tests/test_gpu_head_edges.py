@@ -235,3 +235,54 @@ def test_updates_beside_their_gradients(b, m, n, dtype):
         if m > 1:
             with pytest.raises(SageError):
                 orthogonalize(given, out=buf[:, 1:, first:first + n])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,b,n", [(40, 3, 17), (130, 4, 70), (70, 5, 130), (9, 6, 1)])
+def test_matrices_side_by_side(m, b, n, dtype):
+    """The column slices of one matrix, as a batch: from and to such, in place, and with the result between the slices."""
+    import ctypes
+
+    import torch
+    from paper_2510_02470_amd import binding
+    from paper_2510_02470_amd.binding import SageError, orthogonalize
+
+    g = torch.Generator(device="cuda").manual_seed(n)
+    G = torch.randn(b, m, n, generator=g, device="cuda").to(_tdtype(dtype))
+    want = orthogonalize(G)
+
+    def slices(cols):
+        W = torch.full((m + 1, b * cols + 3), 7.0, dtype=G.dtype, device="cuda")
+        return W, W.as_strided((b, m, cols), (cols, W.stride(0), 1))
+
+    W, given = slices(n)
+    V, out = slices(n)
+    given.copy_(G)
+    assert torch.equal(orthogonalize(given), want)
+    assert torch.equal(orthogonalize(G, out=out), want) and torch.equal(orthogonalize(given, out=out), want) and torch.equal(given, G)
+    assert int((V == 7.0).sum()) >= V.numel() - G.numel()
+    out.fill_(7.0)
+    assert bool((V == 7.0).all())
+    turned = orthogonalize(given.transpose(1, 2))
+    assert torch.equal(turned, want.transpose(1, 2))
+    # one slice with the next one's place for its result
+    W, pairs = slices(2 * n)
+    pairs[:, :, :n].copy_(G)
+    orthogonalize(pairs[:, :, :n], out=pairs[:, :, n:])
+    assert torch.equal(pairs[:, :, n:], want) and torch.equal(pairs[:, :, :n], G)
+    if n > 1:
+        with pytest.raises(SageError):
+            orthogonalize(pairs[:, :, :n], out=pairs[:, :, n - 1:2 * n - 1])
+    orthogonalize(pairs[:, :, :n], out=pairs[:, :, :n])
+    assert torch.equal(pairs[:, :, :n], want)
+    pairs.fill_(7.0)
+    assert bool((W == 7.0).all())
+    # the library's own check of matrices with elements in common
+    L, st = binding.lib(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    work = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    code = binding.SAGE_BF16 if dtype == "bf16" else binding.SAGE_F32
+    p = lambda t: ctypes.c_void_p(t.data_ptr())
+    coef = (ctypes.c_float * 3)(*MUON)
+    res = torch.empty_like(G)
+    for ld, stride in ((b * n, n - 1), (b * n - 1, n)):
+        assert L.sage_orthogonalize(p(G), code, b, m, n, ld, stride, coef, 1, 0.0, 1.0, p(res), n, m * n, p(work), work.numel(), st) == binding.SAGE_ERR_ARG

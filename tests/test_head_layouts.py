@@ -114,3 +114,18 @@ def test_common_elements_of_rows(tmp_path):
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "rows_meet_check ok" in r.stdout, r.stdout
     assert subprocess.run([exe, "spans"], capture_output=True, text=True, timeout=120).returncode == 1
+
+
+def _heads(rows, heads, cols, pad=0):
+    """The column slices of one matrix, as a batch."""
+    return torch.zeros(rows, heads * cols + pad)[:, :heads * cols].view(rows, heads, cols).transpose(0, 1)
+
+
+def test_matrices_side_by_side(recorder):
+    for G, out in ((_heads(6, 4, 9), None), (_heads(6, 4, 9), torch.zeros(4, 6, 9)), (torch.zeros(4, 6, 9), _heads(6, 4, 9)),
+                   (_heads(6, 4, 9, pad=3), _heads(6, 4, 9)), (_heads(9, 4, 6).transpose(1, 2), _heads(9, 4, 6, pad=1).transpose(1, 2)),
+                   (_heads(9, 4, 6).transpose(1, 2), None), (_heads(6, 8, 9)[::2], _heads(6, 4, 9)), (_heads(6, 4, 1), None), (_heads(1, 4, 9), None)):
+        _check(recorder, G, out)
+    for sizes, strides in (((4, 6, 9), (8, 36, 1)), ((4, 6, 9), (9, 35, 1)), ((4, 6, 9), (53, 9, 1)), ((2, 6, 9), (1, 36, 1))):  # with elements in common
+        with pytest.raises(binding.SageError):
+            binding.orthogonalize(torch.zeros(400).as_strided(sizes, strides))
