@@ -286,3 +286,40 @@ def test_matrices_side_by_side(m, b, n, dtype):
     res = torch.empty_like(G)
     for ld, stride in ((b * n, n - 1), (b * n - 1, n)):
         assert L.sage_orthogonalize(p(G), code, b, m, n, ld, stride, coef, 1, 0.0, 1.0, p(res), n, m * n, p(work), work.numel(), st) == binding.SAGE_ERR_ARG
+
+
+# ---- more matrices than the work space takes at once ------------------------------------------------------------
+
+@pytest.mark.parametrize("b,m,n,dtype,pad", [(2400, 1, 513, "f32", 0), (2300, 20, 520, "bf16", 3), (900, 129, 129, "f32", 0), (900, 150, 129, "bf16", 1)])
+def test_batches_in_several_turns(b, m, n, dtype, pad):
+    """Every matrix, the last turn's fewer ones among them, against 64-bit products; what lies between the matrices stays as it was."""
+    import ctypes
+
+    import torch
+    from paper_2510_02470_amd import binding
+
+    code, need = binding.SAGE_BF16 if dtype == "bf16" else binding.SAGE_F32, ctypes.c_size_t(0)
+    sizes = []
+    for count in (b, 2 * b):
+        assert binding.lib().sage_orthogonalize_work(code, count, m, n, ctypes.byref(need)) == binding.SAGE_OK
+        sizes.append(need.value)
+    assert sizes[0] == sizes[1]  # (a turn does not take them all)
+    g = torch.Generator(device="cuda").manual_seed(b + m)
+    G = torch.randn(b, m + pad, n + pad, generator=g, device="cuda").to(_tdtype(dtype))[:, :m, :n]
+    hold = torch.full((b, m + 2 * pad, n + pad), 7.0, dtype=G.dtype, device="cuda")
+    out = hold[:, :m, :n]
+    binding.orthogonalize(G, out=out)
+    X = G.double() if m <= n else G.double().transpose(1, 2).contiguous()
+    X = X / (torch.linalg.vector_norm(X, dim=(1, 2), keepdim=True) + _f32(1e-7))
+    norms = []
+    for _ in range(5):
+        norms.append(float(torch.linalg.vector_norm(X, dim=(1, 2)).max()))
+        A = X @ X.transpose(1, 2).contiguous()
+        X = _f32(MUON[0]) * X + (_f32(MUON[1]) * A + _f32(MUON[2]) * (A @ A)) @ X
+    want = X if m <= n else X.transpose(1, 2)
+    size = torch.linalg.vector_norm(want, dim=(1, 2))
+    tol = ref.orthogonalize_bound(norms, [MUON] * 5, 1.0, m * n) + 1.01 * ref.HALF_STEP[dtype] * size
+    err = torch.linalg.vector_norm(out.double() - want, dim=(1, 2))
+    assert bool((err <= tol).all()), (int((err > tol).nonzero()[0]), float((err / tol).max()))
+    out.fill_(7.0)
+    assert bool((hold == 7.0).all())
