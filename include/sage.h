@@ -390,7 +390,7 @@ int sage_logit_error(const void* logits, sage_dtype dtype, int64_t rows, int64_t
  * ld + cols) or side by side (stride >= cols, (batch - 1) * stride + cols <= ld). SAGE_ERR_ARG also for coefficients under which
  * singular values in [0, 1] pass 2^10 on the way. A zero matrix gives zero.
  * X, A and the polynomial are kept as two fp16 parts, scaled by the bound U of the singular values that the coefficients give (1 before the
- * first step): 22 bits and more of entries above 2^-17 U, 2^-39 U of smaller ones. Products of parts are summed in fp32, the norm in
+ * first step; at least 2^-12): 22 bits and more of entries above 2^-17 U, 2^-39 U of smaller ones. Products of parts are summed in fp32, the norm in
  * fp64. So the result is good to fp32 rounding of the products, for both types, unless eps is so large beside the norm that X
  * itself is below these.
  * work: DEVICE, sage_orthogonalize_work's number of bytes, 256-byte aligned; calls that overlap in time need their own. Its

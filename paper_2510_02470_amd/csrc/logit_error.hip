@@ -17,7 +17,8 @@ namespace sage {
 namespace {
 
 // e^(x - m): the difference is exact or rounded once; the product with log2 e is carried to twice the width where WIDE. Without it a
-// difference of 16 loses 2^-20, which a bf16 E does not show; the sums always have it, for the loss is fp32 whatever E is.
+// difference of 16 loses 2^-20, which a bf16 E does not show; the sums always have it, for the loss is fp32 whatever E is (204 us
+// for 4096 x 65,536 bf16, 198 without it; 410 and 372 for fp32 logits with a bf16 E).
 template <bool WIDE>
 __device__ __forceinline__ float exp_diff(float x, float m) {
     const float d = x - m;
@@ -97,7 +98,7 @@ __device__ __forceinline__ void write_vector(TE* out, int e0, int n, bool whole,
 }
 
 // THREADS threads a row, ROWS rows a work-group (rows of one wave each need no barrier, and a launch of many has fewer work-groups to
-// hand out: 65,536 rows of 1000 bf16 115 us with 256 threads each, 60 with 4 waves for 4 rows). N > 0: N vectors of 16 bytes a thread, kept in
+// hand out: 65,536 rows of 1000 bf16 115 us with 256 threads each, 64 with 4 waves for 4 rows). N > 0: N vectors of 16 bytes a thread, kept in
 // registers between reading and writing; 0: a longer row, read a second time. L: as many vectors more in LDS, where registers alone would
 // leave room for one work-group to a CU, whose reading and writing then have nothing beside them.
 template <class T, class TE, int THREADS, int ROWS, int N, int L>

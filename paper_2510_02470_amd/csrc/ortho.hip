@@ -12,7 +12,7 @@
 //
 // Matrices of up to 64 x 512 have one work-group each and one launch for all steps (ortho_small_kernel). The others take a launch for
 // each product: by tiles of 256 x 256 (only P X, whose tiles are whole), 128 x 128 or 64 x 64, whichever fills the chip (cut_of).
-// 4096 x 4096, five steps: 4.0 ms, 1.03 PFLOP/s of the products that symmetry leaves (the library's plain fp16 product of that size: 1.04).
+// 4096 x 4096, five steps: 4.05 ms, 1.02 PFLOP/s of the products that symmetry leaves (the library's plain fp16 product of that size: 1.04).
 //
 // Layout: 32 columns of a row are 128 bytes, their 32 hi parts and then their 32 lo parts; rows and columns are padded with zeros to
 // multiples of the tiles' side. X is kept row by row for A and column by column for P X: the instructions take both factors along the
@@ -871,8 +871,8 @@ double scale_for(double top) {
 // ortho_wave_kernel, one to a CU, takes 1.0 for four blocks of the summed index and 3 for the rest of a tile of 64 x 64; a tile of
 // 128 x 128 takes 1.0 a block when it has a CU to itself, two on one take 1.6, and 4 for the rest. Tiles that are left over when the slots
 // have been filled as often as possible may be cut along the summed index, so that they fill them too: joining them takes a launch of
-// 6 and 0.03 a part (64 KB written and read). 528 tiles of a 4096 x 4096 product: 275 us as they are, 215 so (512 whole ones
-// and 16 in 32 parts); 48 products X X' of 128 x 1024: 18 in tiles of 128, 11 in tiles of 64.
+// 6 and 0.03 a part (64 KB written and read). 528 tiles of a 4096 x 4096 product: 275 us as they are, 220 so (512 whole ones
+// and 16 in 16 parts); 48 products X X' of 128 x 1024: 18 in tiles of 128, 11 in tiles of 64.
 struct Cut {
     bool waves;  // ortho_wave_kernel
     int splits;  // of the tiles that are left over

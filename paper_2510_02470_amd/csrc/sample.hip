@@ -10,8 +10,9 @@
 // distance to it, and a list of all that is in the K-th's bin and above, on which the rest is done; for top-p without it an approximate
 // histogram of weights and one exact pass; otherwise one exact pass. An exact pass is bound by 64-bit arithmetic: 18 such instructions
 // and about as many others a class, 30 us for a row of 131,072 on a CU, where a reading takes 10. So long bf16 rows without top-k are
-// counted by value, in two passes (draw_by_value). 1024 rows of 131,072 bf16: the greatest 85 us, top-k 50 136, plain 128 (214 by classes),
-// top-p 0.9 135 (410); 37 rows of 50,021 bf16 26 and 32 (31 and 52). A row that has to be left to the other passes costs 7% more.
+// counted by value, in two passes (draw_by_value). 1024 rows of 131,072 bf16, the same ones again and again: the greatest 81 us, top-k 50 135,
+// plain 122 (214 by classes), top-p 0.9 135 (410), 142 on other rows each time; 37 rows of 50,021 bf16 26 and 33 (31 and 52). A row that has
+// to be left to the other passes costs 7% more.
 #include <algorithm>
 #include <type_traits>
 
@@ -527,7 +528,8 @@ __device__ __forceinline__ int draw_listed(const Row<T, THREADS, STAGED>& r, Sha
 // the border of top-p and what min-p leaves are found from values and counts (with 4096 exponentials instead of one for every class), and
 // a second pass adds up a table's entries: 8 instructions a class and a reading of LDS instead of 36. Smaller magnitudes, one in a
 // thousand, are listed; a row with more of them, or with greater ones that matter, is left to the other passes. Both passes treat a class like
-// any other and see to what is not counted once a vector or afterwards: 135 us for 1024 rows of 131,072, 157 with branches for each class.
+// any other and see to what is not counted once a vector or afterwards: 135 us for 1024 rows of 131,072 with top-p, 157 with branches for
+// each class.
 constexpr int VALUES = 4096, HALF = VALUES / 2, MAX_TINY = 1024;
 constexpr unsigned VALUES_FROM = 118u << 7;  // 2^-9
 
@@ -695,7 +697,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : 1) void sample_kernel
     double border = -INFINITY;  // z - m of the least class that min-p keeps; never above 0: the greatest class stays
     if (M32 > 0.f) border = M32 < 1.f ? (double)T32 * log((double)M32) : 0.0;  // (an infinite temperature times ln 1 is no number)
     if constexpr (sizeof(T) == 2 && THREADS >= 512) {
-        // (short rows without top-p take as long either way: 1024 of 16,384 53 us by classes and 54 by values, of 32,768 79 and 68)
+        // (short rows without top-p take as long either way: 1024 of 16,384 51 us by classes and 54 by values, of 32,768 79 and 67)
         if (T32 > 0.f && !(K > 0 && K < C) && (P32 < 1.f || C > 16384)) {
             float m;
             uint64_t total = 0;
